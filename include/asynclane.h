@@ -18,6 +18,10 @@
  *                       drafts, write-back, ordered compaction and
  *                       boundary statistics
  *
+ * and the first two again with the prefix cache and the LM-head weight held in
+ * microscaled 4-bit floating point (mx4_quantize, kv4_store,
+ * lane_attn_forward_kv4, lmhead_confidence_mx4).
+ *
  * Conventions shared by every call
  * --------------------------------
  * - bf16 tensors are passed as uint16_t bit patterns (al_bf16), row-major,
@@ -252,6 +256,121 @@ int lmhead_confidence_noalloc(const al_bf16* hidden, int n_rows,
                               const al_bf16* W, int d, int V,
                               const uint8_t* suppress_eos, int eos_id,
                               float* conf, int32_t* argmax, float* lse, void* stream);
+
+/* ------------------------------------------------------------------------
+ * MXFP4: mx4_quantize + mx4_dequantize.
+ *
+ * Microscaled 4-bit floating point: every 32 consecutive elements of a row are
+ * a block with one scale byte s (e8m0) and 32 e2m1 codes, two to a byte, the
+ * element of lower index in the low nibble.  An element is
+ *     code * 2^(s - 127),   code in {0, 0.5, 1, 1.5, 2, 3, 4, 6}, bit 3 the sign;
+ * s = 255 makes the whole block NaN.
+ *
+ * mx4_quantize: with m the largest magnitude of a block and e = floor(log2 m) - 2
+ * (at least -127; -127 for a block of zeros), s = e + 127 and each code is x / 2^e
+ * rounded to nearest, ties to the even code, magnitudes above 6 (they are below
+ * 8) to 6; the sign of a zero is kept.  A block with an infinity or NaN gets s =
+ * 255 and codes 0.  mx4_dequantize writes the elements in bf16, which holds
+ * them exactly (an element past bf16's range, only met with s >= 253, becomes
+ * an infinity).
+ *
+ * x, y     dev [R][n] bf16;  codes dev [R][n/2] uint8;  scales dev [R][n/32] uint8
+ * R        >= 0 (0 enqueues nothing);  n: multiple of 32, 32..2^30
+ * x, y, codes, scales are 16-byte aligned.
+ * ------------------------------------------------------------------------ */
+int mx4_quantize(const al_bf16* x, long long R, int n, uint8_t* codes, uint8_t* scales, void* stream);
+int mx4_dequantize(const uint8_t* codes, const uint8_t* scales, long long R, int n, al_bf16* y,
+                   void* stream);
+
+/* ------------------------------------------------------------------------
+ * kv4_store -- K/V rows into a prefix cache held in MXFP4.
+ *
+ * The cache of a prefix-sharing group (Section 3.4) with 17/32 byte an element in
+ * place of 2.  It is head-major, so that a head's rows stream; K is plane 0,
+ * V plane 1, each row of D elements in blocks of 32:
+ *     kv_codes dev [2][Hkv][cap][D/2] uint8,  kv_scales dev [2][Hkv][cap][D/32].
+ * (mx4_dequantize with R = 2 * Hkv * cap, n = D reads all of it back.)
+ *
+ * Row r of k and v is quantised as by mx4_quantize into cache row row_idx[r], or
+ * start + r when row_idx is NULL.  A row whose index lies outside [0, cap) is left
+ * out; the cache's other rows keep their contents.  Indices in range must be
+ * unique (not checked).
+ *
+ * k, v     dev [T][Hkv][D] bf16;  T >= 0 (0 enqueues nothing)
+ * row_idx  dev [T] int32 or NULL;  start >= 0, start + T <= cap when row_idx is NULL
+ * cap      >= 1;  Hkv 1..1024;  D: 64 or 128
+ * ------------------------------------------------------------------------ */
+int kv4_store(const al_bf16* k, const al_bf16* v, const int32_t* row_idx, int start, int T,
+              int cap, int Hkv, int D, uint8_t* kv_codes, uint8_t* kv_scales, void* stream);
+
+/* ------------------------------------------------------------------------
+ * lane_attn_forward_kv4 -- lane_attn_forward over a 4-bit prefix cache.
+ *
+ * Which keys a row sees, the softmax, the compact refresh and the refresh-only
+ * call (L = 0) are lane_attn_forward's; the prefix is rows [0, P) of a cache of
+ * kv4_store's layout, whose later rows are not read.  With n_refresh > 0 the rows
+ * k_ref, v_ref are first quantised into rows refresh_idx of the cache (an index
+ * outside [0, P) is left out), then lanes and refreshed rows attend over the
+ * updated values.  The 4-bit values enter both products exactly.
+ *
+ * q, k_lane, v_lane, parent, o, lse, q_ref, k_ref, v_ref, o_ref, lse_ref, scale
+ *          as for lane_attn_forward (bf16; lse fp32 or NULL)
+ * L        0..AL_MAX_LANES;  B: 1..1024, any (1: a single token per lane)
+ * cap      rows of the cache;  P: 0..cap;  n_refresh: 0..P
+ * Hq, Hkv  Hq % Hkv == 0, Hq/Hkv <= 128, Hkv <= 1024;  D: 64 or 128
+ *          L*B*Hq*D < 2^31, n_refresh*Hq < 2^30
+ * kv_codes, kv_scales  may be NULL when P == 0; written only with n_refresh > 0
+ * workspace dev, >= lane_attn_kv4_workspace_size(...) bytes (may be NULL when
+ *          that size is 0); contents need not be initialised
+ * ------------------------------------------------------------------------ */
+size_t lane_attn_kv4_workspace_size(int L, int B, int P, int Hq, int Hkv, int D, int n_refresh);
+
+int lane_attn_forward_kv4(const al_bf16* q, const al_bf16* k_lane, const al_bf16* v_lane,
+                          uint8_t* kv_codes, uint8_t* kv_scales, int cap,
+                          const int32_t* parent, int L, int B, int P,
+                          int Hq, int Hkv, int D, float scale,
+                          const int32_t* refresh_idx, int n_refresh,
+                          const al_bf16* q_ref, const al_bf16* k_ref, const al_bf16* v_ref,
+                          al_bf16* o_ref, float* lse_ref,
+                          al_bf16* o, float* lse,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * LM head on a weight in MXFP4: lmhead_pack_weight_mx4 + lmhead_confidence_mx4.
+ *
+ * lmhead_confidence (Section 3.2) with W the values of an MXFP4 weight; the
+ * hidden rows stay bf16 and products and sums are those of the values (no
+ * rounding of the operands, fp32 accumulation).  The weight is read from a
+ * one-time repacked copy: stages of 128 elements of K, in each stage units of 16
+ * vocabulary rows, in each unit 64 lanes of 16 bytes.  Lane l = 16 b + r of unit
+ * u of stage c holds the 32 codes of row 16 u + r, block 4 c + b, at byte
+ *     ((c * U + u) * 64 + l) * 16,     U = 4 * ceil(V/64) units;
+ * behind all codes, at C * U * 1024 bytes (C = ceil(d/128) stages), the scales,
+ * four units to a dword: unit u's scale for the same row and block is at byte
+ *     ((c * U/4 + u/4) * 64 + l) * 4 + u % 4
+ * of that part.  Rows past V and elements past d are zero.
+ *
+ * lmhead_packed_weight_mx4_size returns the copy's bytes (C * ceil(V/64) * 4352),
+ * 0 for bad arguments.  lmhead_pack_weight_mx4: codes dev [V][d/2], scales dev
+ * [V][d/32] (mx4_quantize's layout) in, W_mx4 dev out (packed_bytes >= that size,
+ * else AL_ERR_WORKSPACE).  lmhead_confidence_mx4: arguments, results and errors
+ * of lmhead_confidence with W_mx4 in place of W, but d is a multiple of 32 (32..
+ * 65536), and the workspace size is lmhead_confidence_mx4_workspace_size(N, d,
+ * V).  Values must be finite; bitwise reproducible from call to call.
+ * ------------------------------------------------------------------------ */
+size_t lmhead_packed_weight_mx4_size(int d, int V);
+
+int lmhead_pack_weight_mx4(const uint8_t* codes, const uint8_t* scales, int d, int V,
+                           uint8_t* W_mx4, size_t packed_bytes, void* stream);
+
+size_t lmhead_confidence_mx4_workspace_size(int N, int d, int V);
+
+int lmhead_confidence_mx4(const al_bf16* hidden, int n_rows,
+                          const int32_t* row_idx, int N,
+                          const uint8_t* W_mx4, int d, int V,
+                          const uint8_t* suppress_eos, int eos_id,
+                          float* conf, int32_t* argmax, float* lse,
+                          void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * select_unmask -- per-lane transfer, lookahead drafts, write-back and

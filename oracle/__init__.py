@@ -16,6 +16,7 @@ attention   lane-batched bidirectional attention over a shared prefix cache,
 lmhead      hidden->vocab logits, max-probability confidence and argmax, in a
             full-softmax form and a chunked online form (Section 3.2, the
             confidence-based transfer rule; refine-lane EOS suppression).
+mx4         microscaled 4-bit floating point: quantiser and values.
 refresh     the compact refresh window length (Section 3.4 "Compact cache
             refresh and reuse").
 scheduler   the active-lane scheduler (Algorithm "AsyncLane active-lane
@@ -25,4 +26,4 @@ select      per-lane confidence-threshold / top-k transfer and the lane
             and step condition (eq. fork_condition), valid prefix length
             (Section 3.2 "Advancement control").
 """
-from . import attention, lmhead, refresh, scheduler, select  # noqa: F401
+from . import attention, lmhead, mx4, refresh, scheduler, select  # noqa: F401

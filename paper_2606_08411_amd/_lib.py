@@ -35,6 +35,7 @@ MAX_SELECT_POSITIONS = 8192
 
 _vp = ctypes.c_void_p
 _i = ctypes.c_int
+_ll = ctypes.c_longlong
 _f = ctypes.c_float
 _sz = ctypes.c_size_t
 
@@ -62,6 +63,17 @@ _SIGNATURES = {
                                       _sz, _vp]),
     "lmhead_confidence_noalloc": (_i, [_vp, _i, _vp, _i, _vp, _i, _i, _vp, _i, _vp, _vp, _vp,
                                        _vp]),
+    "mx4_quantize": (_i, [_vp, _ll, _i, _vp, _vp, _vp]),
+    "mx4_dequantize": (_i, [_vp, _vp, _ll, _i, _vp, _vp]),
+    "kv4_store": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _vp, _vp, _vp]),
+    "lane_attn_kv4_workspace_size": (_sz, [_i] * 7),
+    "lane_attn_forward_kv4": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _vp, _i, _i, _i, _i, _i, _i, _f,
+                                   _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "lmhead_packed_weight_mx4_size": (_sz, [_i, _i]),
+    "lmhead_pack_weight_mx4": (_i, [_vp, _vp, _i, _i, _vp, _sz, _vp]),
+    "lmhead_confidence_mx4_workspace_size": (_sz, [_i, _i, _i]),
+    "lmhead_confidence_mx4": (_i, [_vp, _i, _vp, _i, _vp, _i, _i, _vp, _i, _vp, _vp, _vp, _vp,
+                                   _sz, _vp]),
     "select_unmask": (_i, [_vp, _vp, _vp, _i, _vp, _vp, _i, _i, _vp, _vp, _vp, _i, _f, _i,
                            _vp, _vp, _i, _vp, _i, _vp, _i, _vp, _i, _i, _f, _i, _f,
                            _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
@@ -369,9 +381,10 @@ def lmhead_confidence_workspace_size(N, d, V) -> int:
     return int(library().lmhead_confidence_workspace_size(N, d, V))
 
 
-def _lmhead_args(hidden, W, row_idx, suppress_eos, conf, argmax, lse, want_lse, V=None):
+def _lmhead_args(hidden, W, row_idx, suppress_eos, conf, argmax, lse, want_lse, V=None, mx4=False):
     """Checks and output allocation shared by the LM-head calls.  W is the
-    [V][d] weight, or (V given) the flat packed copy of a [V][d] weight."""
+    [V][d] weight, or (V given) the flat packed copy of a [V][d] weight (mx4: its
+    bytes, of the 4-bit copy)."""
     bf16 = torch.bfloat16
     _tensor(hidden, "hidden", bf16)
     if hidden.dim() != 2:
@@ -382,6 +395,11 @@ def _lmhead_args(hidden, W, row_idx, suppress_eos, conf, argmax, lse, want_lse, 
         if W.dim() != 2 or W.shape[1] != d:
             raise AsyncLaneError(f"W: [V][d={d}] expected, got shape {tuple(W.shape)}")
         V = int(W.shape[0])
+    elif mx4:
+        nbytes = int(library().lmhead_packed_weight_mx4_size(int(d), int(V)))
+        if nbytes == 0:
+            raise AsyncLaneError(f"W_mx4: no packed layout for d={d}, V={V}")
+        _tensor(W, "W_mx4", torch.uint8, min_numel=nbytes)
     else:
         nbytes = int(library().lmhead_packed_weight_size(int(d), int(V)))
         if nbytes == 0:
@@ -577,6 +595,218 @@ def select_unmask(conf, argmax, row_pos, tokens, is_masked, L, B, role, b_len=No
         _ptr(out["delim_flag"]), _stream(tokens))
     _check(st, "select_unmask")
     return out
+
+
+# ------------------------------------------------- 4-bit weights and caches
+def _aligned32(n, name):
+    if n < 32 or n % 32:
+        raise AsyncLaneError(f"{name}: rows of a multiple of 32 elements expected, got {n}")
+    return n
+
+
+def _mx4_pair(codes, scales, names=("codes", "scales")):
+    """Checks codes [..., n/2] against scales [..., n/32]; returns (leading shape, n)."""
+    _tensor(codes, names[0], torch.uint8)
+    if codes.dim() < 1:
+        raise AsyncLaneError(f"{names[0]}: [..., n/2] expected, got shape {tuple(codes.shape)}")
+    lead, n = tuple(codes.shape[:-1]), _aligned32(2 * codes.shape[-1], names[0])
+    _tensor(scales, names[1], torch.uint8, lead + (n // 32,))
+    return lead, n
+
+
+def mx4_quantize(x, codes=None, scales=None):
+    """Rows x [..., n] (bf16, n a multiple of 32) in MXFP4: e2m1 codes
+    [..., n/2] and one scale byte per 32 elements [..., n/32], both uint8.
+    Returns (codes, scales)."""
+    lib = _lib or library()
+    _tensor(x, "x", torch.bfloat16)
+    if x.dim() < 1:
+        raise AsyncLaneError(f"x: [..., n] expected, got shape {tuple(x.shape)}")
+    lead, n = tuple(x.shape[:-1]), _aligned32(x.shape[-1], "x")
+    if codes is None:
+        codes = torch.empty(lead + (n // 2,), dtype=torch.uint8, device=x.device)
+    if scales is None:
+        scales = torch.empty(lead + (n // 32,), dtype=torch.uint8, device=x.device)
+    _tensor(codes, "codes", torch.uint8, lead + (n // 2,))
+    _tensor(scales, "scales", torch.uint8, lead + (n // 32,))
+    _same_device(x, codes, scales)
+    st = _call(lib.mx4_quantize, x, _ptr(x), x.numel() // n, n, _ptr(codes), _ptr(scales), _stream(x))
+    _check(st, "mx4_quantize")
+    return codes, scales
+
+
+def mx4_dequantize(codes, scales, y=None):
+    """The values of MXFP4 rows in bf16 (exact): codes [..., n/2] and scales
+    [..., n/32] (uint8) to y [..., n].  A whole prefix cache of kv4_store is such
+    a pair."""
+    lib = _lib or library()
+    lead, n = _mx4_pair(codes, scales)
+    if y is None:
+        y = torch.empty(lead + (n,), dtype=torch.bfloat16, device=codes.device)
+    _tensor(y, "y", torch.bfloat16, lead + (n,))
+    _same_device(codes, scales, y)
+    st = _call(lib.mx4_dequantize, codes, _ptr(codes), _ptr(scales), y.numel() // n, n, _ptr(y),
+               _stream(codes))
+    _check(st, "mx4_dequantize")
+    return y
+
+
+def _kv4_cache(kv_codes, kv_scales):
+    """Checks a 4-bit cache; returns (Hkv, cap, D)."""
+    _tensor(kv_codes, "kv_codes", torch.uint8)
+    if kv_codes.dim() != 4 or kv_codes.shape[0] != 2:
+        raise AsyncLaneError(f"kv_codes: [2][Hkv][cap][D/2] expected, got shape {tuple(kv_codes.shape)}")
+    _, Hkv, cap, half = kv_codes.shape
+    _tensor(kv_scales, "kv_scales", torch.uint8, (2, Hkv, cap, half // 16))
+    return int(Hkv), int(cap), 2 * int(half)
+
+
+def kv4_store(k, v, kv_codes, kv_scales, row_idx=None, start=0):
+    """Quantise rows k, v [T][Hkv][D] (bf16) into rows row_idx (int32 device
+    tensor [T]; None: start, start + 1, ...) of a 4-bit prefix cache kv_codes
+    [2][Hkv][cap][D/2], kv_scales [2][Hkv][cap][D/32] (uint8, written in place).
+    A row whose index lies outside [0, cap) is left out."""
+    lib = _lib or library()
+    Hkv, cap, D = _kv4_cache(kv_codes, kv_scales)
+    _tensor(k, "k", torch.bfloat16)
+    if k.dim() != 3 or tuple(k.shape[1:]) != (Hkv, D):
+        raise AsyncLaneError(f"k: [T][Hkv={Hkv}][D={D}] expected, got shape {tuple(k.shape)}")
+    T = int(k.shape[0])
+    _tensor(v, "v", torch.bfloat16, k.shape)
+    _tensor(row_idx, "row_idx", torch.int32, (T,), optional=True)
+    _same_device(k, v, kv_codes, kv_scales, row_idx)
+    st = _call(lib.kv4_store, k, _ptr(k), _ptr(v), _ptr(row_idx), int(start), T, cap, Hkv, D,
+               _ptr(kv_codes), _ptr(kv_scales), _stream(k))
+    _check(st, "kv4_store")
+
+
+def lane_attn_kv4_workspace_size(L, B, P, Hq, Hkv, D, n_refresh=0) -> int:
+    return int(library().lane_attn_kv4_workspace_size(L, B, P, Hq, Hkv, D, n_refresh))
+
+
+def lane_attn_forward_kv4(q, k_lane, v_lane, kv_codes, kv_scales, P, parent, B, scale=0.0,
+                          refresh_idx=None, q_ref=None, k_ref=None, v_ref=None,
+                          o=None, lse=None, o_ref=None, lse_ref=None, want_lse=True,
+                          workspace=None):
+    """lane_attn_forward with the prefix in a 4-bit cache (kv4_store's layout),
+    of which rows [0, P) are the prefix.  B may be any number of rows per lane
+    from 1.  Refresh rows are quantised into the cache in place first.  Returns
+    (o, lse, o_ref, lse_ref)."""
+    lib = _lib or library()
+    bf16, f32 = torch.bfloat16, torch.float32
+    Hkv, cap, D = _kv4_cache(kv_codes, kv_scales)
+    P, L = int(P), len(parent)
+    if not 0 <= P <= cap:
+        raise AsyncLaneError(f"P: {P} rows of a cache of {cap}")
+    par = _host_i32(parent, L, "parent")
+    n_ref = 0 if refresh_idx is None else int(refresh_idx.shape[0])
+    dev = kv_codes.device
+    if L > 0:
+        B = int(B)
+        _tensor(q, "q", bf16)
+        if q.dim() != 3 or q.shape[0] != L * B or q.shape[2] != D:
+            raise AsyncLaneError(f"q: [L*B={L * B}][Hq][D={D}] expected, got {tuple(q.shape)}")
+        Hq, LB = int(q.shape[1]), L * B
+        _tensor(k_lane, "k_lane", bf16, (LB, Hkv, D))
+        _tensor(v_lane, "v_lane", bf16, (LB, Hkv, D))
+        if o is None:
+            o = torch.empty_like(q)
+        if lse is None and want_lse:
+            lse = torch.empty((LB, Hq), dtype=f32, device=dev)
+        _tensor(o, "o", bf16, (LB, Hq, D))
+        _tensor(lse, "lse", f32, (LB, Hq), optional=True)
+    else:
+        if n_ref == 0:
+            raise AsyncLaneError("lane_attn_forward_kv4: no lanes and no refresh rows")
+        _tensor(q_ref, "q_ref", bf16)
+        if q_ref.dim() != 3:
+            raise AsyncLaneError(f"q_ref: [n_refresh][Hq][D] expected, got {tuple(q_ref.shape)}")
+        Hq, B = int(q_ref.shape[1]), 1
+    if n_ref:
+        _tensor(refresh_idx, "refresh_idx", torch.int32, (n_ref,))
+        _tensor(q_ref, "q_ref", bf16, (n_ref, Hq, D))
+        _tensor(k_ref, "k_ref", bf16, (n_ref, Hkv, D))
+        _tensor(v_ref, "v_ref", bf16, (n_ref, Hkv, D))
+        if o_ref is None:
+            o_ref = torch.empty_like(q_ref)
+        if lse_ref is None and want_lse:
+            lse_ref = torch.empty((n_ref, Hq), dtype=f32, device=dev)
+        _tensor(o_ref, "o_ref", bf16, (n_ref, Hq, D))
+        _tensor(lse_ref, "lse_ref", f32, (n_ref, Hq), optional=True)
+    _same_device(q, k_lane, v_lane, kv_codes, kv_scales, o, lse, refresh_idx, q_ref, k_ref, v_ref,
+                 o_ref, lse_ref)
+    need = int(lib.lane_attn_kv4_workspace_size(L, B, P, Hq, Hkv, D, n_ref))
+    if workspace is not None:
+        ws, ws_bytes = _explicit_workspace(workspace, dev)
+    stream = _stream(kv_codes)
+    if workspace is None:
+        ws, ws_bytes = _workspace("attn_kv4", need, dev, stream)
+    st = _call(
+        lib.lane_attn_forward_kv4, kv_codes,
+        _ptr(q), _ptr(k_lane), _ptr(v_lane), _ptr(kv_codes), _ptr(kv_scales), cap,
+        _np_ptr(par) if L else None, L, B, P, Hq, Hkv, D, float(scale),
+        _ptr(refresh_idx) if n_ref else None, n_ref,
+        _ptr(q_ref) if n_ref else None, _ptr(k_ref) if n_ref else None,
+        _ptr(v_ref) if n_ref else None, _ptr(o_ref) if n_ref else None,
+        _ptr(lse_ref) if n_ref else None, _ptr(o), _ptr(lse), _ptr(ws), ws_bytes, stream)
+    _check(st, "lane_attn_forward_kv4")
+    return o, lse, o_ref, lse_ref
+
+
+def lmhead_packed_weight_mx4_size(d, V) -> int:
+    return int(library().lmhead_packed_weight_mx4_size(int(d), int(V)))
+
+
+def lmhead_pack_weight_mx4(codes, scales, out=None):
+    """One-time repack of an MXFP4 LM-head weight (mx4_quantize of W [V][d]: codes
+    [V][d/2], scales [V][d/32]) into the layout lmhead_confidence_mx4 streams.
+    Returns a flat uint8 device tensor (or fills `out`)."""
+    lib = library()
+    lead, d = _mx4_pair(codes, scales)
+    if len(lead) != 1:
+        raise AsyncLaneError(f"codes: [V][d/2] expected, got shape {tuple(codes.shape)}")
+    V = int(lead[0])
+    nbytes = int(lib.lmhead_packed_weight_mx4_size(d, V))
+    if nbytes == 0:
+        raise AsyncLaneError(f"codes: unsupported shape {tuple(codes.shape)}")
+    if out is None:
+        out = torch.empty(nbytes, dtype=torch.uint8, device=codes.device)
+    _tensor(out, "out", torch.uint8, min_numel=nbytes)
+    _same_device(codes, scales, out)
+    st = _call(lib.lmhead_pack_weight_mx4, codes, _ptr(codes), _ptr(scales), d, V, _ptr(out), out.numel(),
+               _stream(codes))
+    _check(st, "lmhead_pack_weight_mx4")
+    return out
+
+
+def lmhead_confidence_mx4_workspace_size(N, d, V) -> int:
+    return int(library().lmhead_confidence_mx4_workspace_size(int(N), int(d), int(V)))
+
+
+def lmhead_confidence_mx4(hidden, W_mx4, V, row_idx=None, suppress_eos=None, eos_id=-1,
+                          conf=None, argmax=None, lse=None, want_lse=True, workspace=None):
+    """lmhead_confidence on an MXFP4 weight: W_mx4 is lmhead_pack_weight_mx4's copy
+    of a [V][d] weight, d hidden's width (a multiple of 32).  Returns (conf,
+    argmax, lse)."""
+    lib = _lib or library()
+    V = int(V)
+    n_rows, d, V, N, conf, argmax, lse = _lmhead_args(hidden, W_mx4, row_idx, suppress_eos, conf,
+                                                      argmax, lse, want_lse, V=V, mx4=True)
+    if N == 0:
+        return conf, argmax, lse
+    dev = hidden.device
+    need = int(lib.lmhead_confidence_mx4_workspace_size(N, d, V))
+    if workspace is not None:
+        ws, ws_bytes = _explicit_workspace(workspace, dev)
+    stream = _stream(hidden)
+    if workspace is None:
+        ws, ws_bytes = _workspace("lmhead_mx4", need, dev, stream)
+    st = _call(lib.lmhead_confidence_mx4, hidden,
+               _ptr(hidden), n_rows, _ptr(row_idx), N, _ptr(W_mx4), d, V,
+               _ptr(suppress_eos), int(eos_id), _ptr(conf), _ptr(argmax),
+               _ptr(lse), _ptr(ws), ws_bytes, stream)
+    _check(st, "lmhead_confidence_mx4")
+    return conf, argmax, lse
 
 
 # ------------------------------------------------------------------ scheduler

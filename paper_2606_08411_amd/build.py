@@ -16,7 +16,8 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libasynclane.so")
 FAST = os.path.join(PKG, "_fast.so")   # CPython module (csrc/fast_call.cpp)
-SOURCES = (["abi.cpp", "scheduler.cpp", "lane_attn.hip", "lmhead.hip", "select_unmask.hip"] +
+SOURCES = (["abi.cpp", "scheduler.cpp", "lane_attn.hip", "lane_attn_kv4.hip", "lmhead.hip",
+            "lmhead_mx4.hip", "mx4.hip", "select_unmask.hip"] +
            [f"lmhead_tile_{g}.hip" for g in "abcdefghij"])
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

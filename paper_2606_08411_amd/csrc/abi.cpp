@@ -195,6 +195,122 @@ int lmhead_confidence_noalloc(const al_bf16* hidden, int n_rows, const int32_t* 
                                       argmax, lse, scratch_dev, static_cast<hipStream_t>(stream)));
 }
 
+// ---- MXFP4
+static bool mx4_shape_ok(long long R, int n) {
+  return R >= 0 && n >= 32 && n <= (1 << 30) && n % 32 == 0 && R <= (1ll << 40) / n;
+}
+
+int mx4_quantize(const al_bf16* x, long long R, int n, uint8_t* codes, uint8_t* scales, void* stream) {
+  if (!mx4_shape_ok(R, n)) return AL_ERR_SHAPE;
+  if (R == 0) return AL_OK;
+  if (!x || !codes || !scales) return AL_ERR_NULL;
+  if (!aligned16(x) || !aligned16(codes) || !aligned16(scales)) return AL_ERR_ALIGN;
+  return hip_status(al::launch_mx4_quantize(x, R * n, codes, scales, static_cast<hipStream_t>(stream)));
+}
+
+int mx4_dequantize(const uint8_t* codes, const uint8_t* scales, long long R, int n, al_bf16* y, void* stream) {
+  if (!mx4_shape_ok(R, n)) return AL_ERR_SHAPE;
+  if (R == 0) return AL_OK;
+  if (!y || !codes || !scales) return AL_ERR_NULL;
+  if (!aligned16(y) || !aligned16(codes) || !aligned16(scales)) return AL_ERR_ALIGN;
+  return hip_status(al::launch_mx4_dequantize(codes, scales, R * n, y, static_cast<hipStream_t>(stream)));
+}
+
+int kv4_store(const al_bf16* k, const al_bf16* v, const int32_t* row_idx, int start, int T, int cap, int Hkv, int D,
+              uint8_t* kv_codes, uint8_t* kv_scales, void* stream) {
+  if (T < 0 || cap < 1 || Hkv < 1 || Hkv > 1024 || (D != 64 && D != 128)) return AL_ERR_SHAPE;
+  if (!row_idx && (start < 0 || (long long)start + T > cap)) return AL_ERR_SHAPE;
+  if (T == 0) return AL_OK;
+  if (!k || !v || !kv_codes || !kv_scales) return AL_ERR_NULL;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(kv_codes) || !aligned16(kv_scales) ||
+      (row_idx && !aligned4(row_idx)))
+    return AL_ERR_ALIGN;
+  return hip_status(al::launch_kv4_store(k, v, row_idx, start, T, cap, cap, Hkv, D, kv_codes, kv_scales,
+                                         static_cast<hipStream_t>(stream)));
+}
+
+static bool kv4_shape_ok(int L, int B, int P, int Hq, int Hkv, int D, int n_refresh) {
+  if (L < 0 || L > AL_MAX_LANES || (L == 0 && n_refresh == 0)) return false;   // (L = 0: refresh only)
+  if (L > 0 && (B < 1 || B > 1024)) return false;
+  if (P < 0 || n_refresh < 0 || n_refresh > P) return false;
+  if (Hkv < 1 || Hkv > 1024 || Hq < Hkv || Hq % Hkv != 0 || Hq / Hkv > 128) return false;
+  if (D != 64 && D != 128) return false;
+  if ((L > 0 && (long long)L * B * Hq * D >= (1ll << 31)) || (long long)n_refresh * Hq >= (1ll << 30)) return false;
+  return true;
+}
+
+size_t lane_attn_kv4_workspace_size(int L, int B, int P, int Hq, int Hkv, int D, int n_refresh) {
+  if (!kv4_shape_ok(L, B, P, Hq, Hkv, D, n_refresh)) return 0;
+  return al::kv4_workspace_bytes(L, B, P, Hq, Hkv, D, n_refresh);
+}
+
+int lane_attn_forward_kv4(const al_bf16* q, const al_bf16* k_lane, const al_bf16* v_lane, uint8_t* kv_codes,
+                          uint8_t* kv_scales, int cap, const int32_t* parent, int L, int B, int P, int Hq, int Hkv,
+                          int D, float scale, const int32_t* refresh_idx, int n_refresh, const al_bf16* q_ref,
+                          const al_bf16* k_ref, const al_bf16* v_ref, al_bf16* o_ref, float* lse_ref, al_bf16* o,
+                          float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (L > 0 && (!q || !k_lane || !v_lane || !parent || !o)) return AL_ERR_NULL;
+  if (P > 0 && (!kv_codes || !kv_scales)) return AL_ERR_NULL;
+  if (n_refresh > 0 && (!refresh_idx || !q_ref || !k_ref || !v_ref || !o_ref)) return AL_ERR_NULL;
+  if (!kv4_shape_ok(L, B, P, Hq, Hkv, D, n_refresh) || cap < P) return AL_ERR_SHAPE;
+  if (isnan(scale) || isinf(scale)) return AL_ERR_SHAPE;
+  if ((L > 0 && (!aligned16(q) || !aligned16(k_lane) || !aligned16(v_lane) || !aligned16(o) ||
+                 (lse && !aligned4(lse)))) ||
+      (P > 0 && (!aligned16(kv_codes) || !aligned16(kv_scales))))
+    return AL_ERR_ALIGN;
+  if (n_refresh > 0 && (!aligned16(q_ref) || !aligned16(k_ref) || !aligned16(v_ref) || !aligned16(o_ref) ||
+                        !aligned4(refresh_idx) || (lse_ref && !aligned4(lse_ref))))
+    return AL_ERR_ALIGN;
+  unsigned long long vis[AL_MAX_LANES];
+  const int tree = lane_visibility(parent, L, vis);
+  if (tree != AL_OK) return tree;
+  const size_t need = al::kv4_workspace_bytes(L, B, P, Hq, Hkv, D, n_refresh);
+  if (need > 0) {
+    if (!workspace) return AL_ERR_NULL;
+    if (workspace_bytes < need) return AL_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return AL_ERR_ALIGN;
+  }
+  const float sc = scale > 0.f ? scale : 1.0f / sqrtf((float)D);
+  return hip_status(al::launch_lane_attn_kv4(q, k_lane, v_lane, kv_codes, kv_scales, cap, vis, L, B, P, Hq, Hkv, D, sc,
+                                             refresh_idx, n_refresh, q_ref, k_ref, v_ref, o_ref, lse_ref, o, lse,
+                                             workspace, static_cast<hipStream_t>(stream)));
+}
+
+static bool lm_mx4_shape_ok(int N, int d, int V) { return lm_shape_ok(N, d, V) && d % 32 == 0; }
+
+size_t lmhead_packed_weight_mx4_size(int d, int V) {
+  return lm_mx4_shape_ok(1, d, V) ? al::lmhead_packed_mx4_bytes(d, V) : 0;
+}
+
+int lmhead_pack_weight_mx4(const uint8_t* codes, const uint8_t* scales, int d, int V, uint8_t* W_mx4,
+                           size_t packed_bytes, void* stream) {
+  if (!lm_mx4_shape_ok(1, d, V)) return AL_ERR_SHAPE;
+  if (!codes || !scales || !W_mx4) return AL_ERR_NULL;
+  if (!aligned16(codes) || !aligned16(scales) || !aligned16(W_mx4)) return AL_ERR_ALIGN;
+  if (packed_bytes < al::lmhead_packed_mx4_bytes(d, V)) return AL_ERR_WORKSPACE;
+  return hip_status(al::launch_lmhead_pack_mx4(codes, scales, d, V, W_mx4, static_cast<hipStream_t>(stream)));
+}
+
+size_t lmhead_confidence_mx4_workspace_size(int N, int d, int V) {
+  if (!lm_mx4_shape_ok(N, d, V)) return 0;
+  return al::lmhead_mx4_workspace_bytes(N, V);
+}
+
+int lmhead_confidence_mx4(const al_bf16* hidden, int n_rows, const int32_t* row_idx, int N, const uint8_t* W_mx4,
+                          int d, int V, const uint8_t* suppress_eos, int eos_id, float* conf, int32_t* argmax,
+                          float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (d % 32 != 0) return AL_ERR_SHAPE;
+  bool skip = false;
+  const int st = lmhead_check(hidden, n_rows, row_idx, N, reinterpret_cast<const al_bf16*>(W_mx4), d, V, suppress_eos,
+                              eos_id, conf, argmax, lse, &skip);
+  if (st != AL_OK || skip) return st;
+  if (!workspace) return AL_ERR_NULL;
+  if (workspace_bytes < al::lmhead_mx4_workspace_bytes(N, V)) return AL_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return AL_ERR_ALIGN;
+  return hip_status(al::launch_lmhead_mx4(hidden, row_idx, N, W_mx4, d, V, suppress_eos, eos_id, conf, argmax, lse,
+                                          workspace, static_cast<hipStream_t>(stream)));
+}
+
 int select_unmask(const float* conf, const int32_t* argmax, const int32_t* row_pos, int N,
                   int32_t* tokens, uint8_t* is_masked, int L, int B, const uint8_t* role,
                   const int32_t* b_len, const int32_t* t_lane, int mode, float tau, int fallback_k,

@@ -50,6 +50,31 @@ extern "C" int al_internal_lmhead_plan(int N, int d, int V, int packed, int32_t*
 extern "C" int al_internal_lmhead_instances(int32_t* out, int most);
 hipError_t launch_lmhead_pack(const uint16_t* W, int d, int V, uint16_t* Wp, hipStream_t stream);
 
+// ---- MXFP4: n elements (a multiple of 32) in blocks of 32
+hipError_t launch_mx4_quantize(const uint16_t* x, long long n, uint8_t* codes, uint8_t* scales, hipStream_t stream);
+hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, long long n, uint16_t* y,
+                                 hipStream_t stream);
+// Rows whose index lies outside [0, limit) are left out (limit <= cap).
+hipError_t launch_kv4_store(const uint16_t* k, const uint16_t* v, const int32_t* row_idx, int start, int T, int limit,
+                            int cap, int Hkv, int D, uint8_t* codes, uint8_t* scales, hipStream_t stream);
+
+// ---- lane attention over a 4-bit prefix cache
+size_t kv4_workspace_bytes(int L, int B, int P, int Hq, int Hkv, int D, int n_refresh);
+hipError_t launch_lane_attn_kv4(const uint16_t* q, const uint16_t* k_lane, const uint16_t* v_lane, uint8_t* codes,
+                                uint8_t* scales, int cap, const unsigned long long* vis, int L, int B, int P, int Hq,
+                                int Hkv, int D, float scale, const int32_t* refresh_idx, int n_refresh,
+                                const uint16_t* q_ref, const uint16_t* k_ref, const uint16_t* v_ref, uint16_t* o_ref,
+                                float* lse_ref, uint16_t* o, float* lse, void* ws, hipStream_t stream);
+
+// ---- LM head on a 4-bit weight
+size_t lmhead_mx4_workspace_bytes(int N, int V);
+size_t lmhead_packed_mx4_bytes(int d, int V);
+hipError_t launch_lmhead_pack_mx4(const uint8_t* codes, const uint8_t* scales, int d, int V, uint8_t* out,
+                                  hipStream_t stream);
+hipError_t launch_lmhead_mx4(const uint16_t* hidden, const int32_t* row_idx, int N, const uint8_t* W, int d, int V,
+                             const uint8_t* sup, int eos_id, float* conf, int32_t* argmax, float* lse, void* ws,
+                             hipStream_t stream);
+
 // ---- selection
 constexpr int kSelMaxPositions = 8192;
 constexpr int kSelMaxLanes = 64;

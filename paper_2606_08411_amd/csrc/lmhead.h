@@ -35,6 +35,10 @@ __device__ __forceinline__ void merge_state(float& m, float& s, int& idx, float 
   m = M;
 }
 
+// Combines the partials [column tile][nt_cols][n_vt] of N scored rows (lmhead.hip).
+hipError_t launch_lmhead_merge(const LmPartial* part, int N, int n_vt, int nt_cols, float* conf, int32_t* argmax,
+                               float* lse, hipStream_t stream);
+
 struct LmTileParams {
   const uint16_t* hidden;
   const int32_t* row_idx;

@@ -291,6 +291,13 @@ hipError_t launch_lmhead_pack(const uint16_t* W, int d, int V, uint16_t* Wp, hip
   return hipGetLastError();
 }
 
+hipError_t launch_lmhead_merge(const LmPartial* part, int N, int n_vt, int nt_cols, float* conf, int32_t* argmax,
+                               float* lse, hipStream_t stream) {
+  hipLaunchKernelGGL(lmhead_merge_kernel, dim3(N), dim3(LM_MERGE_THREADS), 0, stream, part, N, n_vt, nt_cols, conf,
+                     argmax, lse);
+  return hipGetLastError();
+}
+
 hipError_t launch_lmhead(const uint16_t* hidden, const int32_t* row_idx, int N,
                          const uint16_t* W, int d, int V, const uint8_t* sup, int eos_id,
                          float* conf, int32_t* argmax, float* lse, void* ws,
@@ -322,9 +329,7 @@ hipError_t launch_lmhead(const uint16_t* hidden, const int32_t* row_idx, int N,
 #undef AL_LM_X
     default: return hipErrorInvalidValue;
   }
-  hipLaunchKernelGGL(lmhead_merge_kernel, dim3(N), dim3(LM_MERGE_THREADS), 0, stream, p.part, N,
-                     L.n_vt, 16 * L.cbt, conf, argmax, lse);
-  return hipGetLastError();
+  return launch_lmhead_merge(p.part, N, L.n_vt, 16 * L.cbt, conf, argmax, lse, stream);
 }
 
 }  // namespace al

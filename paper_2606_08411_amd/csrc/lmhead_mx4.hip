@@ -1,0 +1,309 @@
+// Fused LM head + confidence on a weight in MXFP4 (mx4.h): the computation of
+// lmhead.hip, z[v] = <H[row_idx[n]], W[v]> with W's values the 4-bit ones.  Codes
+// are converted to bf16 in registers (exact) and multiplied by the 16x16x32
+// bf16 MFMA with fp32 accumulation, so the hidden rows keep all their bits.
+//
+// A workgroup is WR x WC wavefronts: wavefront row i owns 64 vocabulary rows
+// (a "unit" of the packed weight, four 16-row MFMA tiles), and the WC columns of
+// wavefronts share out 16 CBT scored rows.  K goes in stages of 128 elements:
+// lane 16 b + r of a wavefront takes the 16 bytes of row r, scale block b, so one
+// dwordx4 load per 16 rows and stage, one scale per lane and four MFMA steps of 8
+// elements a lane (a contraction may walk its index in any order, as long as both
+// operands do).  W goes straight to registers, two stages ahead: no wavefront
+// of the same column needs another's, and LDS carries only the hidden rows.
+//
+// What bounds it: with few columns the W stream (17/32 byte an element, against
+// 2 in bf16), with many the matrix cores.  A stage of a wavefront is 64
+// conversions (~5 cycles each) against 16 x 16 cycles of MFMA per 16 columns.
+#include <math.h>
+
+#include <algorithm>
+
+#include "common.h"
+#include "launch.h"
+#include "lmhead.h"
+#include "mx4.h"
+
+namespace al {
+
+struct LmMx4Params {
+  const uint16_t* hidden;
+  const int32_t* row_idx;
+  const uint8_t* codes;    // [n_st][4 n_u][64][16]
+  const uint8_t* scales;   // [n_st][n_u][64][4]
+  const uint8_t* sup;
+  LmPartial* part;         // [n_nt][16 CBT][n_vt]
+  int N, d, V, eos_id;
+  int n_u, n_st;           // 64-row units, 128-element stages
+  int n_vt, n_nt;          // workgroups over the units (n_u units shared out evenly) and the columns
+};
+
+// Row c of a hidden stage is 256 bytes in LDS, segment s (16 bytes) in slot s ^
+// lm_slot(c): the 16 lanes that one LDS cycle serves (0-3, 12-15, 20-23, 24-27 and
+// so on) then touch every bank once.
+__device__ __forceinline__ int lm_slot(int c) { return (c & 3) | ((c & 8) ? 12 : 0); }
+
+template <int CBT, int WC, int MAXW, bool NT>
+__global__ __launch_bounds__(MAXW * kWave) void lmhead_mx4_kernel(LmMx4Params p) {
+  constexpr int COLS = 16 * CBT;
+  constexpr int CB0 = (CBT + WC - 1) / WC, CB1 = CBT - (WC - 1) * CB0;   // column tiles of the first, last column
+  static_assert(WC == 1 || WC == 2, "at most two columns of wavefronts");
+  constexpr int HB = COLS * 256;          // bytes of the hidden rows of a stage
+  constexpr int NPIECE = COLS / 4;        // 1 KB pieces (4 rows) of a stage
+  __shared__ __attribute__((aligned(1024))) char ring[3 * HB];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n_wave = blockDim.x >> 6;
+  const int wc = WC == 1 ? 0 : w & 1, wr = WC == 1 ? w : w >> 1;
+  const int l16 = lane & 15, kb = lane >> 4;
+  const int nt = blockIdx.x % p.n_nt, vt = blockIdx.x / p.n_nt;
+  const int u_begin = (int)((long long)vt * p.n_u / p.n_vt), u_end = (int)((long long)(vt + 1) * p.n_u / p.n_vt);
+  const int u = min(u_begin + wr, u_end - 1);   // (a wavefront past the tile's units repeats the last one)
+
+  // Hidden rows: piece j of a stage is rows 4 j .. 4 j + 3 of the column tile, by
+  // wavefront j % n_wave.  Elements past d are zero.
+  const unsigned ring0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
+  const char* const zero = reinterpret_cast<const char*>(zero_seg16);
+  auto load_hidden = [&](int st) {
+    const unsigned lds = ring0 + (st % 3) * HB;
+    for (int j = w; j < NPIECE; j += n_wave) {
+      const int c = 4 * j + kb;
+      const int n = min(nt * COLS + c, p.N - 1);
+      const int k = st * 128 + (l16 ^ lm_slot(c)) * 8;
+      const size_t row = p.row_idx ? p.row_idx[n] : n;
+      load_to_lds16<0>(k < p.d ? reinterpret_cast<const char*>(p.hidden + row * p.d + k) : zero, lds + j * 1024);
+    }
+  };
+  struct Stage {
+    i32x4 c[4];
+    unsigned s;
+  };
+  auto load_w = [&](Stage& g, int st) {
+    const i32x4* src = reinterpret_cast<const i32x4*>(p.codes) + ((size_t)st * 4 * p.n_u + 4 * u) * 64 + lane;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) g.c[i] = NT ? __builtin_nontemporal_load(src + i * 64) : src[i * 64];
+    g.s = reinterpret_cast<const unsigned*>(p.scales)[((size_t)st * p.n_u + u) * 64 + lane];
+  };
+
+  auto body = [&](auto nc_tag) {
+    constexpr int NC = decltype(nc_tag)::value;
+    f32x4 acc[4][NC];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < NC; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int brow = (wc * CB0 * 16 + l16) * 256;
+    auto compute = [&](const Stage& g, int st) {
+      const char* b0 = ring + (st % 3) * HB + brow;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        bf16x8 b[NC];
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+          b[j] = *reinterpret_cast<const bf16x8*>(b0 + j * 4096 + (((4 * kb + s) ^ lm_slot(l16)) * 16));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bf16x8 a = mx4_bf16x8((unsigned)g.c[i][s], mx4_scale((g.s >> (8 * i)) & 255));
+#pragma unroll
+          for (int j = 0; j < NC; ++j) acc[i][j] = mfma16x16x32(a, b[j], acc[i][j]);
+        }
+      }
+    };
+    Stage g[3];
+    load_hidden(0);
+    load_w(g[0], 0);
+    if (p.n_st > 1) {
+      load_hidden(1);
+      load_w(g[1], 1);
+    }
+    for (int st = 0; st < p.n_st; st += 3) {
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        if (st + q < p.n_st) {
+          // Everyone's loads of this stage's hidden rows have arrived (all but the
+          // next stage's W loads, issued last), and everyone is done with the
+          // stage before, whose buffer the loads below take.
+          if (st + q + 1 < p.n_st) wait_loads_and_barrier<5>();
+          else wait_loads_and_barrier<0>();
+          if (st + q + 2 < p.n_st) {
+            load_hidden(st + q + 2);
+            load_w(g[(q + 2) % 3], st + q + 2);
+          }
+          compute(g[q], st + q);
+        }
+      }
+    }
+    // Lane (l16, kb) holds vocabulary rows 64 u + 16 i + 4 kb + r of column 16 j + l16.
+    __syncthreads();
+    float* red_m = reinterpret_cast<float*>(ring);
+    float* red_s = red_m + MAXW * COLS / WC;
+    int* red_i = reinterpret_cast<int*>(red_s + MAXW * COLS / WC);
+    const bool mine = u_begin + wr < u_end;
+    const int ve = mine ? min(p.V, (u + 1) * 64) : 0;   // (nothing from a repeated unit)
+    const bool eos_here = p.sup && p.eos_id >= u * 64 && p.eos_id < ve;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const int col = wc * CB0 * 16 + 16 * j + l16;
+      int excl = -1;
+      if (eos_here) {
+        const int n = nt * COLS + col;
+        excl = (n < p.N && p.sup[n]) ? p.eos_id : -1;
+      }
+      float m = -INFINITY;
+      int idx = 0x7fffffff;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int v = u * 64 + 16 * i + 4 * kb + r;
+          const float z = (v < ve && v != excl) ? acc[i][j][r] : -INFINITY;
+          acc[i][j][r] = z;
+          const bool gt = z > m;
+          m = gt ? z : m;
+          idx = gt ? v : idx;
+        }
+      const float m0 = (m == -INFINITY) ? 0.f : m;
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s += exp2_fast((acc[i][j][r] - m0) * LM_LOG2E);
+      merge_state(m, s, idx, __shfl_xor(m, 16, kWave), __shfl_xor(s, 16, kWave), __shfl_xor(idx, 16, kWave));
+      merge_state(m, s, idx, __shfl_xor(m, 32, kWave), __shfl_xor(s, 32, kWave), __shfl_xor(idx, 32, kWave));
+      if (kb == 0) {
+        red_m[wr * COLS + col] = m;
+        red_s[wr * COLS + col] = s;
+        red_i[wr * COLS + col] = idx;
+      }
+    }
+    __syncthreads();
+    const int n_wr = n_wave / WC;
+    for (int col = tid; col < COLS; col += blockDim.x) {
+      float m = red_m[col], s = red_s[col];
+      int idx = red_i[col];
+      for (int i = 1; i < n_wr; ++i) merge_state(m, s, idx, red_m[i * COLS + col], red_s[i * COLS + col], red_i[i * COLS + col]);
+      LmPartial q;
+      q.m = m;
+      q.s = s;
+      q.idx = idx;
+      q.pad = 0;
+      p.part[((size_t)nt * COLS + col) * p.n_vt + vt] = q;
+    }
+  };
+  if (WC == 1 || wc == 0) body(IntTag<CB0>{});
+  else body(IntTag<CB1>{});
+}
+
+// ------------------------------------------------------------------ pack
+// One 16-byte segment of codes per thread (lane 16 b + r of unit-quarter uq, stage
+// c: row 16 uq + r, bytes 64 c + 16 b), then one dword of scales (the four quarters).
+__global__ __launch_bounds__(256) void lmhead_pack_mx4_kernel(const uint8_t* codes, const uint8_t* scales, int d, int V,
+                                                              int n_u, int n_st, uint8_t* out) {
+  const long long n_seg = (long long)n_st * n_u * 256, n_sc = (long long)n_st * n_u * 64;
+  for (long long o = (long long)blockIdx.x * 256 + threadIdx.x; o < n_seg + n_sc; o += (long long)gridDim.x * 256) {
+    if (o < n_seg) {
+      const int l = (int)(o & 63);
+      const long long b = o >> 6;
+      const int uq = (int)(b % (4 * n_u)), c = (int)(b / (4 * n_u));
+      const long long v = 16ll * uq + (l & 15);
+      const int blk = 4 * c + (l >> 4);   // 32-element block of the row
+      i32x4 x = {0, 0, 0, 0};
+      if (v < V && 32 * blk < d) x = *reinterpret_cast<const i32x4*>(codes + v * (d / 2) + 16ll * blk);
+      reinterpret_cast<i32x4*>(out)[o] = x;
+    } else {
+      const long long q = o - n_seg;
+      const int l = (int)(q & 63);
+      const long long b = q >> 6;
+      const int u = (int)(b % n_u), c = (int)(b / n_u);
+      const int blk = 4 * c + (l >> 4);
+      unsigned x = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const long long v = 64ll * u + 16 * i + (l & 15);
+        if (v < V && 32 * blk < d) x |= (unsigned)scales[v * (d / 32) + blk] << (8 * i);
+      }
+      reinterpret_cast<unsigned*>(out + n_seg * 16)[q] = x;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ host
+static int mx4_units(int V) { return (V + 63) / 64; }
+static int mx4_stages(int d) { return (d + 127) / 128; }
+
+size_t lmhead_packed_mx4_bytes(int d, int V) { return (size_t)mx4_stages(d) * mx4_units(V) * (4096 + 256); }
+
+hipError_t launch_lmhead_pack_mx4(const uint8_t* codes, const uint8_t* scales, int d, int V, uint8_t* out,
+                                  hipStream_t stream) {
+  hipLaunchKernelGGL(lmhead_pack_mx4_kernel, dim3(8192), dim3(256), 0, stream, codes, scales, d, V, mx4_units(V),
+                     mx4_stages(d), out);
+  return hipGetLastError();
+}
+
+struct LmMx4Layout {
+  int cbt, wr, n_vt, n_nt;
+};
+
+static LmMx4Layout lm_mx4_layout(int N, int V) {
+  const int frags = (N + 15) / 16, n_u = mx4_units(V);
+  LmMx4Layout L{};
+  L.cbt = frags <= 6 ? frags : frags <= 8 ? 8 : frags <= 10 ? 10 : 13;
+  if (L.cbt == 3) L.cbt = 4;
+  L.n_nt = (frags + L.cbt - 1) / L.cbt;
+  L.wr = L.cbt <= 6 ? 8 : 4;
+  L.n_vt = (n_u + L.wr - 1) / L.wr;
+  return L;
+}
+
+size_t lmhead_mx4_workspace_bytes(int N, int V) {
+  if (N <= 0 || V <= 0) return 0;
+  const LmMx4Layout L = lm_mx4_layout(N, V);
+  return sizeof(LmPartial) * (size_t)L.n_nt * 16 * L.cbt * L.n_vt;
+}
+
+template <int CBT, int WC, int MAXW>
+static void launch_mx4_tile(const LmMx4Params& p, int wr, bool nt, hipStream_t stream) {
+  const dim3 grid((unsigned)p.n_vt * p.n_nt), block(wr * WC * kWave);
+  if (nt) hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, MAXW, true>), grid, block, 0, stream, p);
+  else hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, MAXW, false>), grid, block, 0, stream, p);
+}
+
+hipError_t launch_lmhead_mx4(const uint16_t* hidden, const int32_t* row_idx, int N, const uint8_t* W, int d, int V,
+                             const uint8_t* sup, int eos_id, float* conf, int32_t* argmax, float* lse, void* ws,
+                             hipStream_t stream) {
+  if (N <= 0) return hipSuccess;
+  const LmMx4Layout L = lm_mx4_layout(N, V);
+  LmMx4Params p{};
+  p.hidden = hidden;
+  p.row_idx = row_idx;
+  p.n_u = mx4_units(V);
+  p.n_st = mx4_stages(d);
+  p.codes = W;
+  p.scales = W + (size_t)p.n_st * p.n_u * 4096;
+  p.sup = sup;
+  p.part = static_cast<LmPartial*>(ws);
+  p.N = N;
+  p.d = d;
+  p.V = V;
+  p.eos_id = eos_id;
+  p.n_vt = L.n_vt;
+  p.n_nt = L.n_nt;
+  const bool nt = L.n_nt == 1;
+  switch (L.cbt) {
+    case 1: launch_mx4_tile<1, 1, 8>(p, L.wr, nt, stream); break;
+    case 2: launch_mx4_tile<2, 1, 8>(p, L.wr, nt, stream); break;
+    case 4: launch_mx4_tile<4, 1, 8>(p, L.wr, nt, stream); break;
+    case 5: launch_mx4_tile<5, 1, 8>(p, L.wr, nt, stream); break;
+    case 6: launch_mx4_tile<6, 1, 8>(p, L.wr, nt, stream); break;
+    case 8: launch_mx4_tile<8, 2, 8>(p, L.wr, nt, stream); break;
+    case 10: launch_mx4_tile<10, 2, 8>(p, L.wr, nt, stream); break;
+    case 13: launch_mx4_tile<13, 2, 8>(p, L.wr, nt, stream); break;
+    default: return hipErrorInvalidValue;
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  return launch_lmhead_merge(p.part, N, L.n_vt, 16 * L.cbt, conf, argmax, lse, stream);
+}
+
+}  // namespace al
