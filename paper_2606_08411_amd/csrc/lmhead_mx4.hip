@@ -43,36 +43,49 @@ struct LmMx4Params {
 // so on) then touch every bank once.
 __device__ __forceinline__ int lm_slot(int c) { return (c & 3) | ((c & 8) ? 12 : 0); }
 
-template <int CBT, int WC, int MAXW, bool NT>
-__global__ __launch_bounds__(MAXW * kWave) void lmhead_mx4_kernel(LmMx4Params p) {
+template <int CBT, int WC, int DEPTH, bool NT>
+__global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
   constexpr int COLS = 16 * CBT;
   constexpr int CB0 = (CBT + WC - 1) / WC, CB1 = CBT - (WC - 1) * CB0;   // column tiles of the first, last column
   static_assert(WC == 1 || WC == 2, "at most two columns of wavefronts");
-  constexpr int HB = COLS * 256;          // bytes of the hidden rows of a stage
-  constexpr int NPIECE = COLS / 4;        // 1 KB pieces (4 rows) of a stage
-  __shared__ __attribute__((aligned(1024))) char ring[3 * HB];
+  constexpr int HB = COLS * 256;             // bytes of the hidden rows of a stage
+  constexpr int MAXW = 8, TH = MAXW * kWave;
+  constexpr int NH = (COLS * 16 + TH - 1) / TH;   // 16-byte segments of them per thread
+  __shared__ __attribute__((aligned(1024))) char ring[2 * HB];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n_wave = blockDim.x >> 6;
   const int wc = WC == 1 ? 0 : w & 1, wr = WC == 1 ? w : w >> 1;
   const int l16 = lane & 15, kb = lane >> 4;
   const int nt = blockIdx.x % p.n_nt, vt = blockIdx.x / p.n_nt;
   const int u_begin = (int)((long long)vt * p.n_u / p.n_vt), u_end = (int)((long long)(vt + 1) * p.n_u / p.n_vt);
   const int u = min(u_begin + wr, u_end - 1);   // (a wavefront past the tile's units repeats the last one)
 
-  // Hidden rows: piece j of a stage is rows 4 j .. 4 j + 3 of the column tile, by
-  // wavefront j % n_wave.  Elements past d are zero.
-  const unsigned ring0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
-  const char* const zero = reinterpret_cast<const char*>(zero_seg16);
-  auto load_hidden = [&](int st) {
-    const unsigned lds = ring0 + (st % 3) * HB;
-    for (int j = w; j < NPIECE; j += n_wave) {
-      const int c = 4 * j + kb;
-      const int n = min(nt * COLS + c, p.N - 1);
-      const int k = st * 128 + (l16 ^ lm_slot(c)) * 8;
-      const size_t row = p.row_idx ? p.row_idx[n] : n;
-      load_to_lds16<0>(k < p.d ? reinterpret_cast<const char*>(p.hidden + row * p.d + k) : zero, lds + j * 1024);
+  // Hidden rows: thread tid holds segment tid % 16 of rows tid / 16 + i TH / 16 of
+  // the column tile.  Elements past d are zero.
+  unsigned hoff[NH];   // (n_rows * d < 2^31)
+#pragma unroll
+  for (int i = 0; i < NH; ++i) {
+    const int n = min(nt * COLS + (tid >> 4) + i * (TH / 16), p.N - 1);
+    hoff[i] = (unsigned)(p.row_idx ? p.row_idx[n] : n) * (unsigned)p.d + (tid & 15) * 8;
+  }
+  struct Hidden {
+    i32x4 x[NH];
+  };
+  auto load_hidden = [&](Hidden& h, int st) {
+    const bool in = st * 128 + (tid & 15) * 8 < p.d;
+    const uint16_t* src = p.hidden + st * 128;
+#pragma unroll
+    for (int i = 0; i < NH; ++i)
+      h.x[i] = in ? *reinterpret_cast<const i32x4*>(src + hoff[i]) : i32x4{0, 0, 0, 0};
+  };
+  auto store_hidden = [&](const Hidden& h, int st) {
+    char* dst = ring + (st & 1) * HB;
+#pragma unroll
+    for (int i = 0; i < NH; ++i) {
+      const int c = (tid >> 4) + i * (TH / 16);
+      if (NH * TH == COLS * 16 || c < COLS)
+        *reinterpret_cast<i32x4*>(dst + c * 256 + ((tid & 15) ^ lm_slot(c & 15)) * 16) = h.x[i];
     }
   };
   struct Stage {
@@ -93,49 +106,69 @@ __global__ __launch_bounds__(MAXW * kWave) void lmhead_mx4_kernel(LmMx4Params p)
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < NC; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // Step s (8 elements a lane) of a stage: 4 NC MFMAs, in groups of a row tile
+    // i.  While a group runs, the next group's codes are converted and a quarter of
+    // the next step's hidden fragments are read (ROLL: read in the step's last group,
+    // each into the register that its last product has freed).
+    constexpr bool ROLL = CBT > 10;
+    constexpr int RPG = (NC + 3) / 4, NB = ROLL ? 1 : 2;
     const int brow = (wc * CB0 * 16 + l16) * 256;
     auto compute = [&](const Stage& g, int st) {
-      const char* b0 = ring + (st % 3) * HB + brow;
+      const char* b0 = ring + (st & 1) * HB + brow;
+      bf16x8 b[NB][NC], a[2];
+      auto read_b = [&](int s, int j) {
+        b[s % NB][j] = *reinterpret_cast<const bf16x8*>(b0 + j * 4096 + (((4 * kb + s) ^ lm_slot(l16)) * 16));
+      };
+      auto convert = [&](int q) {   // group q = 4 s + i
+        a[q & 1] = mx4_bf16x8((unsigned)g.c[q & 3][q >> 2], mx4_scale((g.s >> (8 * (q & 3))) & 255));
+      };
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        bf16x8 b[NC];
+      for (int j = 0; j < NC; ++j) read_b(0, j);
+      convert(0);
 #pragma unroll
-        for (int j = 0; j < NC; ++j)
-          b[j] = *reinterpret_cast<const bf16x8*>(b0 + j * 4096 + (((4 * kb + s) ^ lm_slot(l16)) * 16));
+      for (int q = 0; q < 16; ++q) {
+        const int s = q >> 2, i = q & 3;
+        if (s < 3 && !ROLL) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const bf16x8 a = mx4_bf16x8((unsigned)g.c[i][s], mx4_scale((g.s >> (8 * i)) & 255));
-#pragma unroll
-          for (int j = 0; j < NC; ++j) acc[i][j] = mfma16x16x32(a, b[j], acc[i][j]);
+          for (int j = i * RPG; j < (i + 1) * RPG; ++j)
+            if (j < NC) read_b(s + 1, j);
         }
+        if (q < 15) convert(q + 1);
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+          acc[i][j] = mfma16x16x32(a[q & 1], b[s % NB][j], acc[i][j]);
+          if (ROLL && s < 3 && i == 3) read_b(s + 1, j);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     };
-    Stage g[3];
-    load_hidden(0);
-    load_w(g[0], 0);
-    if (p.n_st > 1) {
-      load_hidden(1);
-      load_w(g[1], 1);
-    }
-    for (int st = 0; st < p.n_st; st += 3) {
+    // In a stage the next one's hidden rows go from registers to LDS, the ones after
+    // are loaded, and the codes DEPTH - 1 stages ahead.
+    Stage g[DEPTH];
+    Hidden h;
+    load_hidden(h, 0);
 #pragma unroll
-      for (int q = 0; q < 3; ++q) {
-        if (st + q < p.n_st) {
-          // Everyone's loads of this stage's hidden rows have arrived (all but the
-          // next stage's W loads, issued last), and everyone is done with the
-          // stage before, whose buffer the loads below take.
-          if (st + q + 1 < p.n_st) wait_loads_and_barrier<5>();
-          else wait_loads_and_barrier<0>();
-          if (st + q + 2 < p.n_st) {
-            load_hidden(st + q + 2);
-            load_w(g[(q + 2) % 3], st + q + 2);
-          }
-          compute(g[q], st + q);
+    for (int q = 0; q < DEPTH - 1; ++q) load_w(g[q], min(q, p.n_st - 1));
+    store_hidden(h, 0);
+    if (p.n_st > 1) load_hidden(h, 1);
+    __syncthreads();
+    for (int st = 0; st < p.n_st; st += DEPTH) {
+#pragma unroll
+      for (int q = 0; q < DEPTH; ++q) {
+        const int at = st + q;
+        if (at < p.n_st) {
+          if (at + 1 < p.n_st) store_hidden(h, at + 1);
+          if (at + 2 < p.n_st) load_hidden(h, at + 2);
+          if (at + DEPTH - 1 < p.n_st) load_w(g[(q + DEPTH - 1) % DEPTH], at + DEPTH - 1);
+          __builtin_amdgcn_sched_barrier(0);
+          compute(g[q], at);
+          // (__syncthreads would also wait for the loads)
+          asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         }
       }
     }
+    // (After the last barrier nobody reads the ring.)
     // Lane (l16, kb) holds vocabulary rows 64 u + 16 i + 4 kb + r of column 16 j + l16.
-    __syncthreads();
     float* red_m = reinterpret_cast<float*>(ring);
     float* red_s = red_m + MAXW * COLS / WC;
     int* red_i = reinterpret_cast<int*>(red_s + MAXW * COLS / WC);
@@ -178,11 +211,10 @@ __global__ __launch_bounds__(MAXW * kWave) void lmhead_mx4_kernel(LmMx4Params p)
       }
     }
     __syncthreads();
-    const int n_wr = n_wave / WC;
-    for (int col = tid; col < COLS; col += blockDim.x) {
+    for (int col = tid; col < COLS; col += TH) {
       float m = red_m[col], s = red_s[col];
       int idx = red_i[col];
-      for (int i = 1; i < n_wr; ++i) merge_state(m, s, idx, red_m[i * COLS + col], red_s[i * COLS + col], red_i[i * COLS + col]);
+      for (int i = 1; i < MAXW / WC; ++i) merge_state(m, s, idx, red_m[i * COLS + col], red_s[i * COLS + col], red_i[i * COLS + col]);
       LmPartial q;
       q.m = m;
       q.s = s;
@@ -262,11 +294,11 @@ size_t lmhead_mx4_workspace_bytes(int N, int V) {
   return sizeof(LmPartial) * (size_t)L.n_nt * 16 * L.cbt * L.n_vt;
 }
 
-template <int CBT, int WC, int MAXW>
-static void launch_mx4_tile(const LmMx4Params& p, int wr, bool nt, hipStream_t stream) {
-  const dim3 grid((unsigned)p.n_vt * p.n_nt), block(wr * WC * kWave);
-  if (nt) hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, MAXW, true>), grid, block, 0, stream, p);
-  else hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, MAXW, false>), grid, block, 0, stream, p);
+template <int CBT, int WC, int DEPTH>
+static void launch_mx4_tile(const LmMx4Params& p, bool nt, hipStream_t stream) {
+  const dim3 grid((unsigned)p.n_vt * p.n_nt), block(512);
+  if (nt) hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, DEPTH, true>), grid, block, 0, stream, p);
+  else hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, DEPTH, false>), grid, block, 0, stream, p);
 }
 
 hipError_t launch_lmhead_mx4(const uint16_t* hidden, const int32_t* row_idx, int N, const uint8_t* W, int d, int V,
@@ -291,14 +323,14 @@ hipError_t launch_lmhead_mx4(const uint16_t* hidden, const int32_t* row_idx, int
   p.n_nt = L.n_nt;
   const bool nt = L.n_nt == 1;
   switch (L.cbt) {
-    case 1: launch_mx4_tile<1, 1, 8>(p, L.wr, nt, stream); break;
-    case 2: launch_mx4_tile<2, 1, 8>(p, L.wr, nt, stream); break;
-    case 4: launch_mx4_tile<4, 1, 8>(p, L.wr, nt, stream); break;
-    case 5: launch_mx4_tile<5, 1, 8>(p, L.wr, nt, stream); break;
-    case 6: launch_mx4_tile<6, 1, 8>(p, L.wr, nt, stream); break;
-    case 8: launch_mx4_tile<8, 2, 8>(p, L.wr, nt, stream); break;
-    case 10: launch_mx4_tile<10, 2, 8>(p, L.wr, nt, stream); break;
-    case 13: launch_mx4_tile<13, 2, 8>(p, L.wr, nt, stream); break;
+    case 1: launch_mx4_tile<1, 1, 3>(p, nt, stream); break;
+    case 2: launch_mx4_tile<2, 1, 3>(p, nt, stream); break;
+    case 4: launch_mx4_tile<4, 1, 3>(p, nt, stream); break;
+    case 5: launch_mx4_tile<5, 1, 3>(p, nt, stream); break;
+    case 6: launch_mx4_tile<6, 1, 3>(p, nt, stream); break;
+    case 8: launch_mx4_tile<8, 2, 3>(p, nt, stream); break;
+    case 10: launch_mx4_tile<10, 2, 3>(p, nt, stream); break;
+    case 13: launch_mx4_tile<13, 2, 2>(p, nt, stream); break;
     default: return hipErrorInvalidValue;
   }
   const hipError_t e = hipGetLastError();
