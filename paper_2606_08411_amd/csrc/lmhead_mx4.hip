@@ -43,15 +43,15 @@ struct LmMx4Params {
 // so on) then touch every bank once.
 __device__ __forceinline__ int lm_slot(int c) { return (c & 3) | ((c & 8) ? 12 : 0); }
 
-template <int CBT, int WC, int DEPTH, bool NT>
+template <int CBT, int WC, int DEPTH, int G, bool RAGGED, bool NT>
 __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
   constexpr int COLS = 16 * CBT;
   constexpr int CB0 = (CBT + WC - 1) / WC, CB1 = CBT - (WC - 1) * CB0;   // column tiles of the first, last column
   static_assert(WC == 1 || WC == 2, "at most two columns of wavefronts");
   constexpr int HB = COLS * 256;             // bytes of the hidden rows of a stage
   constexpr int MAXW = 8, TH = MAXW * kWave;
-  constexpr int NH = (COLS * 16 + TH - 1) / TH;   // 16-byte segments of them per thread
-  __shared__ __attribute__((aligned(1024))) char ring[2 * HB];
+  constexpr int LH = (COLS / 4 + MAXW - 1) / MAXW;       // direct loads of them per wavefront
+  __shared__ __attribute__((aligned(1024))) char ring[3 * G * HB];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -61,31 +61,31 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
   const int u_begin = (int)((long long)vt * p.n_u / p.n_vt), u_end = (int)((long long)(vt + 1) * p.n_u / p.n_vt);
   const int u = min(u_begin + wr, u_end - 1);   // (a wavefront past the tile's units repeats the last one)
 
-  // Hidden rows: thread tid holds segment tid % 16 of rows tid / 16 + i TH / 16 of
-  // the column tile.  Elements past d are zero.
-  unsigned hoff[NH];   // (n_rows * d < 2^31)
+  // Hidden rows go straight to LDS, in pieces of 1 KB (4 rows): piece w + 8 i by
+  // wavefront w (the last one again where there are none left, so that every
+  // wavefront has LH loads a stage).  Elements past d are zero.
+  const unsigned ring0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
+  unsigned hoff[LH];   // bytes (n_rows * d < 2^31)
 #pragma unroll
-  for (int i = 0; i < NH; ++i) {
-    const int n = min(nt * COLS + (tid >> 4) + i * (TH / 16), p.N - 1);
-    hoff[i] = (unsigned)(p.row_idx ? p.row_idx[n] : n) * (unsigned)p.d + (tid & 15) * 8;
+  for (int i = 0; i < LH; ++i) {
+    const int c = 4 * min(w + 8 * i, COLS / 4 - 1) + kb;
+    const int n = min(nt * COLS + c, p.N - 1);
+    hoff[i] = 2 * (unsigned)(p.row_idx ? p.row_idx[n] : n) * (unsigned)p.d + (l16 ^ lm_slot(c & 15)) * 16;
   }
-  struct Hidden {
-    i32x4 x[NH];
-  };
-  auto load_hidden = [&](Hidden& h, int st) {
-    const bool in = st * 128 + (tid & 15) * 8 < p.d;
-    const uint16_t* src = p.hidden + st * 128;
+  // (Stages past the last load from the first: the loads of a stage are always the
+  // same number and need no branch, so every wait counts them exactly.)
+  auto load_hidden = [&](int st, int slot) {
+    const char* src = reinterpret_cast<const char*>(p.hidden) + (size_t)(st < p.n_st ? st : 0) * 256;
 #pragma unroll
-    for (int i = 0; i < NH; ++i)
-      h.x[i] = in ? *reinterpret_cast<const i32x4*>(src + hoff[i]) : i32x4{0, 0, 0, 0};
-  };
-  auto store_hidden = [&](const Hidden& h, int st) {
-    char* dst = ring + (st & 1) * HB;
-#pragma unroll
-    for (int i = 0; i < NH; ++i) {
-      const int c = (tid >> 4) + i * (TH / 16);
-      if (NH * TH == COLS * 16 || c < COLS)
-        *reinterpret_cast<i32x4*>(dst + c * 256 + ((tid & 15) ^ lm_slot(c & 15)) * 16) = h.x[i];
+    for (int i = 0; i < LH; ++i) {
+      const int piece = min(w + 8 * i, COLS / 4 - 1);
+      const unsigned lds_at = ring0 + slot + piece * 1024;
+      if (RAGGED) {
+        const int k = st * 128 + (l16 ^ lm_slot((4 * piece + kb) & 15)) * 8;
+        load_to_lds16<0>(k < p.d ? src + hoff[i] : reinterpret_cast<const char*>(zero_seg16), lds_at);
+      } else {
+        load_to_lds16<0, 0, false>(uniform_ptr(src), hoff[i], lds_at);
+      }
     }
   };
   struct Stage {
@@ -93,10 +93,11 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
     unsigned s;
   };
   auto load_w = [&](Stage& g, int st) {
-    const i32x4* src = reinterpret_cast<const i32x4*>(p.codes) + ((size_t)st * 4 * p.n_u + 4 * u) * 64 + lane;
+    const size_t at = st < p.n_st ? (size_t)st * p.n_u + u : 0;
+    const i32x4* src = reinterpret_cast<const i32x4*>(p.codes) + at * 256 + lane;
 #pragma unroll
     for (int i = 0; i < 4; ++i) g.c[i] = NT ? __builtin_nontemporal_load(src + i * 64) : src[i * 64];
-    g.s = reinterpret_cast<const unsigned*>(p.scales)[((size_t)st * p.n_u + u) * 64 + lane];
+    g.s = reinterpret_cast<const unsigned*>(p.scales)[at * 64 + lane];
   };
 
   auto body = [&](auto nc_tag) {
@@ -113,8 +114,8 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
     constexpr bool ROLL = CBT > 10;
     constexpr int RPG = (NC + 3) / 4, NB = ROLL ? 1 : 2;
     const int brow = (wc * CB0 * 16 + l16) * 256;
-    auto compute = [&](const Stage& g, int st) {
-      const char* b0 = ring + (st & 1) * HB + brow;
+    auto compute = [&](const Stage& g, int slot) {
+      const char* b0 = ring + slot + brow;
       bf16x8 b[NB][NC], a[2];
       auto read_b = [&](int s, int j) {
         b[s % NB][j] = *reinterpret_cast<const bf16x8*>(b0 + j * 4096 + (((4 * kb + s) ^ lm_slot(l16)) * 16));
@@ -142,31 +143,40 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    // In a stage the next one's hidden rows go from registers to LDS, the ones after
-    // are loaded, and the codes DEPTH - 1 stages ahead.
+    // G stages are a group, with one barrier: at its top the group's hidden rows have
+    // arrived (all but the loads issued after them: W of two groups and the hidden
+    // rows of one), everyone is done with the group before, and its buffer takes
+    // the hidden rows of the group after next.
     Stage g[DEPTH];
-    Hidden h;
-    load_hidden(h, 0);
 #pragma unroll
-    for (int q = 0; q < DEPTH - 1; ++q) load_w(g[q], min(q, p.n_st - 1));
-    store_hidden(h, 0);
-    if (p.n_st > 1) load_hidden(h, 1);
-    __syncthreads();
-    for (int st = 0; st < p.n_st; st += DEPTH) {
+    for (int q = 0; q < DEPTH - 1; ++q) {
+      load_w(g[q], q);
+      asm volatile("" ::: "memory");   // (in this order, which the waits in the loop assume)
+    }
+    int slot = 0;   // byte of the ring
+    auto next_slot = [&](int x, int by) {
+      x += by * G * HB;
+      return x >= 3 * G * HB ? x - 3 * G * HB : x;
+    };
 #pragma unroll
-      for (int q = 0; q < DEPTH; ++q) {
-        const int at = st + q;
-        if (at < p.n_st) {
-          if (at + 1 < p.n_st) store_hidden(h, at + 1);
-          if (at + 2 < p.n_st) load_hidden(h, at + 2);
-          if (at + DEPTH - 1 < p.n_st) load_w(g[(q + DEPTH - 1) % DEPTH], at + DEPTH - 1);
-          __builtin_amdgcn_sched_barrier(0);
-          compute(g[q], at);
-          // (__syncthreads would also wait for the loads)
-          asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    for (int i = 0; i < 2 * G; ++i) load_hidden(i, i * HB);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    constexpr int UNROLL = DEPTH % G ? DEPTH * G : DEPTH;
+    for (int st = 0; st < p.n_st; st += UNROLL) {
+#pragma unroll
+      for (int q = 0; q < UNROLL; ++q) {
+        if (q % G == 0) {
+          wait_loads_and_barrier<10 * G + G * LH>();
+#pragma unroll
+          for (int i = 0; i < G; ++i) load_hidden(st + q + 2 * G + i, next_slot(slot, 2) + i * HB);
         }
+        load_w(g[(q + DEPTH - 1) % DEPTH], st + q + DEPTH - 1);
+        __builtin_amdgcn_sched_barrier(0);
+        if (st + q < p.n_st) compute(g[q % DEPTH], slot + q % G * HB);
+        if (q % G == G - 1) slot = next_slot(slot, 1);
       }
     }
+    wait_loads_and_barrier<0>();   // (the last loads land in the ring too)
     // (After the last barrier nobody reads the ring.)
     // Lane (l16, kb) holds vocabulary rows 64 u + 16 i + 4 kb + r of column 16 j + l16.
     float* red_m = reinterpret_cast<float*>(ring);
@@ -294,11 +304,15 @@ size_t lmhead_mx4_workspace_bytes(int N, int V) {
   return sizeof(LmPartial) * (size_t)L.n_nt * 16 * L.cbt * L.n_vt;
 }
 
-template <int CBT, int WC, int DEPTH>
+template <int CBT, int WC, int DEPTH, int G>
 static void launch_mx4_tile(const LmMx4Params& p, bool nt, hipStream_t stream) {
   const dim3 grid((unsigned)p.n_vt * p.n_nt), block(512);
-  if (nt) hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, DEPTH, true>), grid, block, 0, stream, p);
-  else hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, DEPTH, false>), grid, block, 0, stream, p);
+  if (p.d % 128)
+    hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, DEPTH, G, true, false>), grid, block, 0, stream, p);
+  else if (nt)
+    hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, DEPTH, G, false, true>), grid, block, 0, stream, p);
+  else
+    hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, DEPTH, G, false, false>), grid, block, 0, stream, p);
 }
 
 hipError_t launch_lmhead_mx4(const uint16_t* hidden, const int32_t* row_idx, int N, const uint8_t* W, int d, int V,
@@ -323,14 +337,14 @@ hipError_t launch_lmhead_mx4(const uint16_t* hidden, const int32_t* row_idx, int
   p.n_nt = L.n_nt;
   const bool nt = L.n_nt == 1;
   switch (L.cbt) {
-    case 1: launch_mx4_tile<1, 1, 3>(p, nt, stream); break;
-    case 2: launch_mx4_tile<2, 1, 3>(p, nt, stream); break;
-    case 4: launch_mx4_tile<4, 1, 3>(p, nt, stream); break;
-    case 5: launch_mx4_tile<5, 1, 3>(p, nt, stream); break;
-    case 6: launch_mx4_tile<6, 1, 3>(p, nt, stream); break;
-    case 8: launch_mx4_tile<8, 2, 3>(p, nt, stream); break;
-    case 10: launch_mx4_tile<10, 2, 3>(p, nt, stream); break;
-    case 13: launch_mx4_tile<13, 2, 2>(p, nt, stream); break;
+    case 1: launch_mx4_tile<1, 1, 4, 2>(p, nt, stream); break;
+    case 2: launch_mx4_tile<2, 1, 4, 2>(p, nt, stream); break;
+    case 4: launch_mx4_tile<4, 1, 4, 2>(p, nt, stream); break;
+    case 5: launch_mx4_tile<5, 1, 3, 1>(p, nt, stream); break;
+    case 6: launch_mx4_tile<6, 1, 3, 1>(p, nt, stream); break;
+    case 8: launch_mx4_tile<8, 2, 3, 1>(p, nt, stream); break;
+    case 10: launch_mx4_tile<10, 2, 3, 1>(p, nt, stream); break;
+    case 13: launch_mx4_tile<13, 2, 2, 1>(p, nt, stream); break;
     default: return hipErrorInvalidValue;
   }
   const hipError_t e = hipGetLastError();
