@@ -293,7 +293,7 @@ int lmhead_pack_weight_mx4(const uint8_t* codes, const uint8_t* scales, int d, i
 
 size_t lmhead_confidence_mx4_workspace_size(int N, int d, int V) {
   if (!lm_mx4_shape_ok(N, d, V)) return 0;
-  return al::lmhead_mx4_workspace_bytes(N, V);
+  return al::lmhead_mx4_workspace_bytes(N, d, V);
 }
 
 int lmhead_confidence_mx4(const al_bf16* hidden, int n_rows, const int32_t* row_idx, int N, const uint8_t* W_mx4,
@@ -305,7 +305,7 @@ int lmhead_confidence_mx4(const al_bf16* hidden, int n_rows, const int32_t* row_
                               eos_id, conf, argmax, lse, &skip);
   if (st != AL_OK || skip) return st;
   if (!workspace) return AL_ERR_NULL;
-  if (workspace_bytes < al::lmhead_mx4_workspace_bytes(N, V)) return AL_ERR_WORKSPACE;
+  if (workspace_bytes < al::lmhead_mx4_workspace_bytes(N, d, V)) return AL_ERR_WORKSPACE;
   if (!aligned16(workspace)) return AL_ERR_ALIGN;
   return hip_status(al::launch_lmhead_mx4(hidden, row_idx, N, W_mx4, d, V, suppress_eos, eos_id, conf, argmax, lse,
                                           workspace, static_cast<hipStream_t>(stream)));

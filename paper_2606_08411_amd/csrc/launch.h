@@ -67,7 +67,7 @@ hipError_t launch_lane_attn_kv4(const uint16_t* q, const uint16_t* k_lane, const
                                 float* lse_ref, uint16_t* o, float* lse, void* ws, hipStream_t stream);
 
 // ---- LM head on a 4-bit weight
-size_t lmhead_mx4_workspace_bytes(int N, int V);
+size_t lmhead_mx4_workspace_bytes(int N, int d, int V);
 size_t lmhead_packed_mx4_bytes(int d, int V);
 hipError_t launch_lmhead_pack_mx4(const uint8_t* codes, const uint8_t* scales, int d, int V, uint8_t* out,
                                   hipStream_t stream);

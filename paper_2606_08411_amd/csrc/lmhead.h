@@ -35,6 +35,9 @@ __device__ __forceinline__ void merge_state(float& m, float& s, int& idx, float 
   m = M;
 }
 
+// Compute units of the current device (cached per device).
+int lm_cu_count();
+
 // Combines the partials [column tile][nt_cols][n_vt] of N scored rows (lmhead.hip).
 hipError_t launch_lmhead_merge(const LmPartial* part, int N, int n_vt, int nt_cols, float* conf, int32_t* argmax,
                                float* lse, hipStream_t stream);

@@ -75,7 +75,7 @@ __global__ __launch_bounds__(LM_MERGE_THREADS) void lmhead_merge_kernel(
 
 // ------------------------------------------------------------------ host
 // Compute units of the current device (cached per device).
-static int lm_cu_count() {
+int lm_cu_count() {
   static int cached[64];
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;

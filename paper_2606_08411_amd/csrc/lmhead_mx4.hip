@@ -26,6 +26,8 @@
 
 namespace al {
 
+constexpr int LM_MX4_WAVES = 8;
+
 struct LmMx4Params {
   const uint16_t* hidden;
   const int32_t* row_idx;
@@ -43,45 +45,47 @@ struct LmMx4Params {
 // so on) then touch every bank once.
 __device__ __forceinline__ int lm_slot(int c) { return (c & 3) | ((c & 8) ? 12 : 0); }
 
-template <int CBT, int WC, int DEPTH, int G, bool RAGGED, bool NT>
+template <int CBT, int WC, int KS, int DEPTH, bool RAGGED, bool NT>
 __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
   constexpr int COLS = 16 * CBT;
   constexpr int CB0 = (CBT + WC - 1) / WC, CB1 = CBT - (WC - 1) * CB0;   // column tiles of the first, last column
-  static_assert(WC == 1 || WC == 2, "at most two columns of wavefronts");
+  static_assert(WC == 1 || (WC == 2 && KS == 1), "at most two columns of wavefronts");
+  constexpr int WR = LM_MX4_WAVES / (WC * KS), TH = LM_MX4_WAVES * kWave;
   constexpr int HB = COLS * 256;             // bytes of the hidden rows of a stage
-  constexpr int MAXW = 8, TH = MAXW * kWave;
-  constexpr int LH = (COLS / 4 + MAXW - 1) / MAXW;       // direct loads of them per wavefront
-  __shared__ __attribute__((aligned(1024))) char ring[3 * G * HB];
+  constexpr int LH = (KS * COLS / 4 + LM_MX4_WAVES - 1) / LM_MX4_WAVES;   // direct loads of a group per wavefront
+  __shared__ __attribute__((aligned(1024))) char ring[3 * KS * HB];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wc = WC == 1 ? 0 : w & 1, wr = WC == 1 ? w : w >> 1;
+  const int wc = WC == 1 ? 0 : w & 1, ks = w % KS, wr = w / (WC * KS);
   const int l16 = lane & 15, kb = lane >> 4;
   const int nt = blockIdx.x % p.n_nt, vt = blockIdx.x / p.n_nt;
   const int u_begin = (int)((long long)vt * p.n_u / p.n_vt), u_end = (int)((long long)(vt + 1) * p.n_u / p.n_vt);
-  const int u = min(u_begin + wr, u_end - 1);   // (a wavefront past the tile's units repeats the last one)
+  const int u = u_begin + wr;
+  const bool active = u < u_end;   // (a wavefront past the tile's units loads hidden rows only)
 
-  // Hidden rows go straight to LDS, in pieces of 1 KB (4 rows): piece w + 8 i by
-  // wavefront w (the last one again where there are none left, so that every
-  // wavefront has LH loads a stage).  Elements past d are zero.
+  // Hidden rows go straight to LDS, in pieces of 1 KB (4 rows of a stage): pieces w + 8
+  // i of a group of KS stages by wavefront w (the last one again where there are
+  // none left, so that every wavefront has LH loads a group).  Elements past d are
+  // zero.  (Stages past the last load from the first: the loads of a group are
+  // always the same number and need no branch, so every wait counts them exactly.)
   const unsigned ring0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
   unsigned hoff[LH];   // bytes (n_rows * d < 2^31)
+  auto piece = [&](int i) { return min(w + LM_MX4_WAVES * i, KS * COLS / 4 - 1); };
 #pragma unroll
   for (int i = 0; i < LH; ++i) {
-    const int c = 4 * min(w + 8 * i, COLS / 4 - 1) + kb;
+    const int c = 4 * (piece(i) % (COLS / 4)) + kb;
     const int n = min(nt * COLS + c, p.N - 1);
     hoff[i] = 2 * (unsigned)(p.row_idx ? p.row_idx[n] : n) * (unsigned)p.d + (l16 ^ lm_slot(c & 15)) * 16;
   }
-  // (Stages past the last load from the first: the loads of a stage are always the
-  // same number and need no branch, so every wait counts them exactly.)
-  auto load_hidden = [&](int st, int slot) {
-    const char* src = reinterpret_cast<const char*>(p.hidden) + (size_t)(st < p.n_st ? st : 0) * 256;
+  auto load_hidden = [&](int group, int slot) {
 #pragma unroll
     for (int i = 0; i < LH; ++i) {
-      const int piece = min(w + 8 * i, COLS / 4 - 1);
-      const unsigned lds_at = ring0 + slot + piece * 1024;
+      const int st = group * KS + piece(i) / (COLS / 4);
+      const char* src = reinterpret_cast<const char*>(p.hidden) + (size_t)(st < p.n_st ? st : 0) * 256;
+      const unsigned lds_at = ring0 + slot + piece(i) * 1024;
       if (RAGGED) {
-        const int k = st * 128 + (l16 ^ lm_slot((4 * piece + kb) & 15)) * 8;
+        const int k = st * 128 + (l16 ^ lm_slot((4 * piece(i) + kb) & 15)) * 8;
         load_to_lds16<0>(k < p.d ? src + hoff[i] : reinterpret_cast<const char*>(zero_seg16), lds_at);
       } else {
         load_to_lds16<0, 0, false>(uniform_ptr(src), hoff[i], lds_at);
@@ -143,88 +147,123 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    // G stages are a group, with one barrier: at its top the group's hidden rows have
-    // arrived (all but the loads issued after them: W of two groups and the hidden
-    // rows of one), everyone is done with the group before, and its buffer takes
-    // the hidden rows of the group after next.
-    Stage g[DEPTH];
-#pragma unroll
-    for (int q = 0; q < DEPTH - 1; ++q) {
-      load_w(g[q], q);
-      asm volatile("" ::: "memory");   // (in this order, which the waits in the loop assume)
-    }
+    // Group i is stages KS i .. KS i + KS - 1, of which this wavefront multiplies stage
+    // KS i + ks.  At the barrier on its top the group's hidden rows have arrived (all
+    // but the loads issued after them: W twice and one group of hidden rows),
+    // everyone is done with the group before, and its buffer takes the hidden rows
+    // of the group after next.
+    const int n_group = (p.n_st + KS - 1) / KS;
     int slot = 0;   // byte of the ring
     auto next_slot = [&](int x, int by) {
-      x += by * G * HB;
-      return x >= 3 * G * HB ? x - 3 * G * HB : x;
+      x += by * KS * HB;
+      return x >= 3 * KS * HB ? x - 3 * KS * HB : x;
     };
-#pragma unroll
-    for (int i = 0; i < 2 * G; ++i) load_hidden(i, i * HB);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    constexpr int UNROLL = DEPTH % G ? DEPTH * G : DEPTH;
-    for (int st = 0; st < p.n_st; st += UNROLL) {
-#pragma unroll
-      for (int q = 0; q < UNROLL; ++q) {
-        if (q % G == 0) {
-          wait_loads_and_barrier<10 * G + G * LH>();
-#pragma unroll
-          for (int i = 0; i < G; ++i) load_hidden(st + q + 2 * G + i, next_slot(slot, 2) + i * HB);
-        }
-        load_w(g[(q + DEPTH - 1) % DEPTH], st + q + DEPTH - 1);
-        __builtin_amdgcn_sched_barrier(0);
-        if (st + q < p.n_st) compute(g[q % DEPTH], slot + q % G * HB);
-        if (q % G == G - 1) slot = next_slot(slot, 1);
+    if (!active) {
+      load_hidden(0, 0);
+      load_hidden(1, KS * HB);
+      for (int i = 0; i < n_group; ++i) {
+        wait_loads_and_barrier<LH>();
+        load_hidden(i + 2, next_slot(slot, 2));
+        slot = next_slot(slot, 1);
       }
+    } else {
+      Stage g[DEPTH];
+#pragma unroll
+      for (int q = 0; q < DEPTH - 1; ++q) {
+        load_w(g[q], q * KS + ks);
+        asm volatile("" ::: "memory");   // (in this order, which the waits in the loop assume)
+      }
+      load_hidden(0, 0);
+      load_hidden(1, KS * HB);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      for (int i0 = 0;; i0 += DEPTH) {   // (left from inside: no paths with fewer loads meet in it)
+#pragma unroll
+        for (int q = 0; q < DEPTH; ++q) {
+          const int i = i0 + q;
+          if (i >= n_group) goto done;
+          wait_loads_and_barrier<10 + LH>();
+          load_hidden(i + 2, next_slot(slot, 2));
+          load_w(g[(q + DEPTH - 1) % DEPTH], (i + DEPTH - 1) * KS + ks);
+          __builtin_amdgcn_sched_barrier(0);
+          if (KS == 1 || i * KS + ks < p.n_st) compute(g[q], slot + ks * HB);
+          slot = next_slot(slot, 1);
+        }
+      }
+    done:;
     }
     wait_loads_and_barrier<0>();   // (the last loads land in the ring too)
-    // (After the last barrier nobody reads the ring.)
+    // The KS partial sums of a tile, in ascending order of ks.
+    if (KS > 1) {
+      f32x4* sum = reinterpret_cast<f32x4*>(ring) + (size_t)wr * (KS - 1) * 4 * NC * 64 + lane;
+      if (active && ks > 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < NC; ++j) sum[((ks - 1) * 4 * NC + i * NC + j) * 64] = acc[i][j];
+      }
+      __syncthreads();
+      if (active && ks == 0) {
+        for (int k = 0; k < KS - 1; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < NC; ++j) {
+              const f32x4 v = sum[(k * 4 * NC + i * NC + j) * 64];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[i][j][e] += v[e];
+            }
+      }
+      __syncthreads();
+    }
     // Lane (l16, kb) holds vocabulary rows 64 u + 16 i + 4 kb + r of column 16 j + l16.
     float* red_m = reinterpret_cast<float*>(ring);
-    float* red_s = red_m + MAXW * COLS / WC;
-    int* red_i = reinterpret_cast<int*>(red_s + MAXW * COLS / WC);
-    const bool mine = u_begin + wr < u_end;
-    const int ve = mine ? min(p.V, (u + 1) * 64) : 0;   // (nothing from a repeated unit)
-    const bool eos_here = p.sup && p.eos_id >= u * 64 && p.eos_id < ve;
+    float* red_s = red_m + WR * COLS;
+    int* red_i = reinterpret_cast<int*>(red_s + WR * COLS);
+    if (active && ks == 0) {
+      const int ve = min(p.V, (u + 1) * 64);
+      const bool eos_here = p.sup && p.eos_id >= u * 64 && p.eos_id < ve;
 #pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      const int col = wc * CB0 * 16 + 16 * j + l16;
-      int excl = -1;
-      if (eos_here) {
-        const int n = nt * COLS + col;
-        excl = (n < p.N && p.sup[n]) ? p.eos_id : -1;
-      }
-      float m = -INFINITY;
-      int idx = 0x7fffffff;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int v = u * 64 + 16 * i + 4 * kb + r;
-          const float z = (v < ve && v != excl) ? acc[i][j][r] : -INFINITY;
-          acc[i][j][r] = z;
-          const bool gt = z > m;
-          m = gt ? z : m;
-          idx = gt ? v : idx;
+      for (int j = 0; j < NC; ++j) {
+        const int col = wc * CB0 * 16 + 16 * j + l16;
+        int excl = -1;
+        if (eos_here) {
+          const int n = nt * COLS + col;
+          excl = (n < p.N && p.sup[n]) ? p.eos_id : -1;
         }
-      const float m0 = (m == -INFINITY) ? 0.f : m;
-      float s = 0.f;
+        float m = -INFINITY;
+        int idx = 0x7fffffff;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s += exp2_fast((acc[i][j][r] - m0) * LM_LOG2E);
-      merge_state(m, s, idx, __shfl_xor(m, 16, kWave), __shfl_xor(s, 16, kWave), __shfl_xor(idx, 16, kWave));
-      merge_state(m, s, idx, __shfl_xor(m, 32, kWave), __shfl_xor(s, 32, kWave), __shfl_xor(idx, 32, kWave));
-      if (kb == 0) {
-        red_m[wr * COLS + col] = m;
-        red_s[wr * COLS + col] = s;
-        red_i[wr * COLS + col] = idx;
+          for (int r = 0; r < 4; ++r) {
+            const int v = u * 64 + 16 * i + 4 * kb + r;
+            const float z = (v < ve && v != excl) ? acc[i][j][r] : -INFINITY;
+            acc[i][j][r] = z;
+            const bool gt = z > m;
+            m = gt ? z : m;
+            idx = gt ? v : idx;
+          }
+        const float m0 = (m == -INFINITY) ? 0.f : m;
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s += exp2_fast((acc[i][j][r] - m0) * LM_LOG2E);
+        merge_state(m, s, idx, __shfl_xor(m, 16, kWave), __shfl_xor(s, 16, kWave), __shfl_xor(idx, 16, kWave));
+        merge_state(m, s, idx, __shfl_xor(m, 32, kWave), __shfl_xor(s, 32, kWave), __shfl_xor(idx, 32, kWave));
+        if (kb == 0) {
+          red_m[wr * COLS + col] = m;
+          red_s[wr * COLS + col] = s;
+          red_i[wr * COLS + col] = idx;
+        }
       }
     }
     __syncthreads();
     for (int col = tid; col < COLS; col += TH) {
       float m = red_m[col], s = red_s[col];
       int idx = red_i[col];
-      for (int i = 1; i < MAXW / WC; ++i) merge_state(m, s, idx, red_m[i * COLS + col], red_s[i * COLS + col], red_i[i * COLS + col]);
+      for (int i = 1; i < u_end - u_begin; ++i)
+        merge_state(m, s, idx, red_m[i * COLS + col], red_s[i * COLS + col], red_i[i * COLS + col]);
       LmPartial q;
       q.m = m;
       q.s = s;
@@ -283,43 +322,69 @@ hipError_t launch_lmhead_pack_mx4(const uint8_t* codes, const uint8_t* scales, i
   return hipGetLastError();
 }
 
+// The instances built, X(CBT, WC, KS, DEPTH): 16 CBT columns, WC columns of
+// wavefronts, K split over KS wavefronts, W loaded DEPTH - 1 stages ahead.  One
+// unit row of wavefronts is 8 / (WC KS) units.  A wavefront's 16 CBT / WC fp32 sums, DEPTH
+// x 17 registers of W and the fragments have to fit 256 registers, three groups of
+// hidden rows (12 KS CBT KB) the LDS.
+#define AL_LM_MX4_INSTANCES(X) \
+  X(1, 1, 1, 4) X(2, 1, 1, 4) X(4, 1, 1, 4) X(5, 1, 1, 3) X(6, 1, 1, 3) X(8, 2, 1, 3) X(10, 2, 1, 3) X(13, 2, 1, 3) \
+  X(1, 1, 8, 4) X(2, 1, 4, 4) X(4, 1, 2, 4) X(5, 1, 2, 3) X(6, 1, 2, 3)
+
 struct LmMx4Layout {
-  int cbt, wr, n_vt, n_nt;
+  int cbt, wc, ks, n_vt, n_nt;
 };
 
-static LmMx4Layout lm_mx4_layout(int N, int V) {
-  const int frags = (N + 15) / 16, n_u = mx4_units(V);
-  LmMx4Layout L{};
-  L.cbt = frags <= 6 ? frags : frags <= 8 ? 8 : frags <= 10 ? 10 : 13;
-  if (L.cbt == 3) L.cbt = 4;
-  L.n_nt = (frags + L.cbt - 1) / L.cbt;
-  L.wr = L.cbt <= 6 ? 8 : 4;
-  L.n_vt = (n_u + L.wr - 1) / L.wr;
-  return L;
+// The cheapest instance: n_nt column tiles, and either whole rounds of workgroups of
+// as many units as there are unit rows, or one round with the units shared out over
+// all compute units.
+static LmMx4Layout lm_mx4_layout(int N, int d, int V) {
+  const int frags = (N + 15) / 16, n_u = mx4_units(V), n_st = mx4_stages(d), cus = lm_cu_count();
+  LmMx4Layout best{};
+  double best_t = 1e30;
+#define AL_LM_MX4_TRY(CBT, WC, KS, DEPTH)                                                          \
+  {                                                                                                \
+    const int wr = LM_MX4_WAVES / (WC * KS), n_nt = (frags + CBT - 1) / CBT;                       \
+    const int n_vt = std::max((n_u + wr - 1) / wr, std::min(n_u, std::max(1, cus / n_nt)));        \
+    const int upw = (n_u + n_vt - 1) / n_vt;                                                       \
+    const double waves = (upw * WC * KS + 3) / 4;                                                  \
+    const double stage = std::max(0.45, waves * (0.25 + 0.16 * ((CBT + WC - 1) / WC)));            \
+    const double rounds = (double)(((long long)n_vt * n_nt + cus - 1) / cus);                      \
+    const double t = rounds * (((n_st + KS - 1) / KS) * stage + 3.0 + (KS > 1 ? 1.0 : 0.0)) * (1 + 0.05 * (n_nt - 1)); \
+    if (t < best_t) {                                                                              \
+      best_t = t;                                                                                  \
+      best = LmMx4Layout{CBT, WC, KS, n_vt, n_nt};                                                 \
+    }                                                                                              \
+  }
+#define AL_LM_MX4_X(CBT, WC, KS, DEPTH) AL_LM_MX4_TRY(CBT, WC, KS, DEPTH)
+  AL_LM_MX4_INSTANCES(AL_LM_MX4_X)
+#undef AL_LM_MX4_X
+#undef AL_LM_MX4_TRY
+  return best;
 }
 
-size_t lmhead_mx4_workspace_bytes(int N, int V) {
+size_t lmhead_mx4_workspace_bytes(int N, int d, int V) {
   if (N <= 0 || V <= 0) return 0;
-  const LmMx4Layout L = lm_mx4_layout(N, V);
+  const LmMx4Layout L = lm_mx4_layout(N, d, V);
   return sizeof(LmPartial) * (size_t)L.n_nt * 16 * L.cbt * L.n_vt;
 }
 
-template <int CBT, int WC, int DEPTH, int G>
+template <int CBT, int WC, int KS, int DEPTH>
 static void launch_mx4_tile(const LmMx4Params& p, bool nt, hipStream_t stream) {
-  const dim3 grid((unsigned)p.n_vt * p.n_nt), block(512);
+  const dim3 grid((unsigned)p.n_vt * p.n_nt), block(LM_MX4_WAVES * kWave);
   if (p.d % 128)
-    hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, DEPTH, G, true, false>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, KS, DEPTH, true, false>), grid, block, 0, stream, p);
   else if (nt)
-    hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, DEPTH, G, false, true>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, KS, DEPTH, false, true>), grid, block, 0, stream, p);
   else
-    hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, DEPTH, G, false, false>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((lmhead_mx4_kernel<CBT, WC, KS, DEPTH, false, false>), grid, block, 0, stream, p);
 }
 
 hipError_t launch_lmhead_mx4(const uint16_t* hidden, const int32_t* row_idx, int N, const uint8_t* W, int d, int V,
                              const uint8_t* sup, int eos_id, float* conf, int32_t* argmax, float* lse, void* ws,
                              hipStream_t stream) {
   if (N <= 0) return hipSuccess;
-  const LmMx4Layout L = lm_mx4_layout(N, V);
+  const LmMx4Layout L = lm_mx4_layout(N, d, V);
   LmMx4Params p{};
   p.hidden = hidden;
   p.row_idx = row_idx;
@@ -336,15 +401,11 @@ hipError_t launch_lmhead_mx4(const uint16_t* hidden, const int32_t* row_idx, int
   p.n_vt = L.n_vt;
   p.n_nt = L.n_nt;
   const bool nt = L.n_nt == 1;
-  switch (L.cbt) {
-    case 1: launch_mx4_tile<1, 1, 4, 2>(p, nt, stream); break;
-    case 2: launch_mx4_tile<2, 1, 4, 2>(p, nt, stream); break;
-    case 4: launch_mx4_tile<4, 1, 4, 2>(p, nt, stream); break;
-    case 5: launch_mx4_tile<5, 1, 3, 1>(p, nt, stream); break;
-    case 6: launch_mx4_tile<6, 1, 3, 1>(p, nt, stream); break;
-    case 8: launch_mx4_tile<8, 2, 3, 1>(p, nt, stream); break;
-    case 10: launch_mx4_tile<10, 2, 3, 1>(p, nt, stream); break;
-    case 13: launch_mx4_tile<13, 2, 2, 1>(p, nt, stream); break;
+  switch (L.cbt * 64 + L.wc * 16 + L.ks) {
+#define AL_LM_MX4_X(CBT, WC, KS, DEPTH) \
+  case CBT * 64 + WC * 16 + KS: launch_mx4_tile<CBT, WC, KS, DEPTH>(p, nt, stream); break;
+    AL_LM_MX4_INSTANCES(AL_LM_MX4_X)
+#undef AL_LM_MX4_X
     default: return hipErrorInvalidValue;
   }
   const hipError_t e = hipGetLastError();
