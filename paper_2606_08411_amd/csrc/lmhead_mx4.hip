@@ -97,7 +97,8 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
     unsigned s;
   };
   auto load_w = [&](Stage& g, int st) {
-    const size_t at = st < p.n_st ? (size_t)st * p.n_u + u : 0;
+    const int in = st < p.n_st;
+    const size_t at = (size_t)(in ? st : 0) * p.n_u + (in ? u : 0);
     const i32x4* src = reinterpret_cast<const i32x4*>(p.codes) + at * 256 + lane;
 #pragma unroll
     for (int i = 0; i < 4; ++i) g.c[i] = NT ? __builtin_nontemporal_load(src + i * 64) : src[i * 64];
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
     // but the loads issued after them: W twice and one group of hidden rows),
     // everyone is done with the group before, and its buffer takes the hidden rows
     // of the group after next.
-    const int n_group = (p.n_st + KS - 1) / KS;
+    const int n_group = (p.n_st + KS - 1) / KS, n_run = (n_group + DEPTH - 1) / DEPTH * DEPTH;
     int slot = 0;   // byte of the ring
     auto next_slot = [&](int x, int by) {
       x += by * KS * HB;
@@ -161,7 +162,7 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
     if (!active) {
       load_hidden(0, 0);
       load_hidden(1, KS * HB);
-      for (int i = 0; i < n_group; ++i) {
+      for (int i = 0; i < n_run; ++i) {
         wait_loads_and_barrier<LH>();
         load_hidden(i + 2, next_slot(slot, 2));
         slot = next_slot(slot, 1);
@@ -176,20 +177,18 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
       load_hidden(0, 0);
       load_hidden(1, KS * HB);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      for (int i0 = 0;; i0 += DEPTH) {   // (left from inside: no paths with fewer loads meet in it)
+      for (int i0 = 0; i0 < n_run; i0 += DEPTH) {
 #pragma unroll
         for (int q = 0; q < DEPTH; ++q) {
           const int i = i0 + q;
-          if (i >= n_group) goto done;
           wait_loads_and_barrier<10 + LH>();
           load_hidden(i + 2, next_slot(slot, 2));
           load_w(g[(q + DEPTH - 1) % DEPTH], (i + DEPTH - 1) * KS + ks);
           __builtin_amdgcn_sched_barrier(0);
-          if (KS == 1 || i * KS + ks < p.n_st) compute(g[q], slot + ks * HB);
+          if (i * KS + ks < p.n_st) compute(g[q], slot + ks * HB);
           slot = next_slot(slot, 1);
         }
       }
-    done:;
     }
     wait_loads_and_barrier<0>();   // (the last loads land in the ring too)
     // The KS partial sums of a tile, in ascending order of ks.
@@ -350,7 +349,7 @@ static LmMx4Layout lm_mx4_layout(int N, int d, int V) {
     const double waves = (upw * WC * KS + 3) / 4;                                                  \
     const double stage = std::max(0.45, waves * (0.25 + 0.16 * ((CBT + WC - 1) / WC)));            \
     const double rounds = (double)(((long long)n_vt * n_nt + cus - 1) / cus);                      \
-    const double t = rounds * (((n_st + KS - 1) / KS) * stage + 3.0 + (KS > 1 ? 1.0 : 0.0)) * (1 + 0.05 * (n_nt - 1)); \
+    const double t = rounds * (((n_st + KS - 1) / KS) * stage + 3.0 + (KS > 1 ? 2.5 : 0.0)) * (1 + 0.1 * (n_nt - 1));  \
     if (t < best_t) {                                                                              \
       best_t = t;                                                                                  \
       best = LmMx4Layout{CBT, WC, KS, n_vt, n_nt};                                                 \
