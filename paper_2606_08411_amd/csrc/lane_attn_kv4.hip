@@ -29,10 +29,14 @@
 
 namespace al {
 
-constexpr int K4_KT = 64;            // keys per tile
-constexpr int K4_WAVES = 8;          // query tiles per workgroup
+constexpr int K4_KT = 64;            // keys per tile of the tile kernel
+constexpr int K4_UT = 32;            // keys per unit of the unit kernel
+constexpr int K4_WAVES = 8;
 constexpr int K4_THREADS = K4_WAVES * kWave;
 constexpr float K4_LN2 = 0.6931471805599453f;
+// A pair's reference maximum moves only when a tile's scores exceed it by more than
+// this many powers of two, so O is rescaled in few tiles.
+constexpr float K4_RESCALE_LOG2 = 8.0f;
 
 struct Kv4Params {
   const uint16_t* q;        // [n_rows][Hq][D]
@@ -46,15 +50,17 @@ struct Kv4Params {
   float* part_ml;           // [n_split][n_rows * Hq][2]
   int n_rows, R, B, P, cap, Hq, Hkv, g;
   int n_pairs;              // n_rows * g
-  int n_pre, n_tiles, n_split;   // prefix tiles, all key tiles
+  int n_pre, n_tiles, n_split;   // prefix tiles (units), all key tiles (units)
+  int tpw;                  // tile kernel: query tiles (computing wavefronts) per workgroup
   float scale_log2;
   unsigned long long vis[64];    // bit j: lane block j visible to lane i
 };
 
-// Bits of the 64 lane rows from `row` on that a pair with visibility v sees.
+// Bits of the KT lane rows from `row` on that a pair with visibility v sees.
+template <int KT>
 __device__ __forceinline__ unsigned long long key_mask(unsigned long long v, int row, int B, int R) {
   unsigned long long m = 0;
-  const int end = min(row + K4_KT, R);
+  const int end = min(row + KT, R);
   for (int j = row / B; j * B < end; ++j) {   // (uniform)
     const int a = max(j * B - row, 0), b = min((j + 1) * B, end) - row;
     const unsigned long long bits = (b >= 64 ? ~0ull : (1ull << b) - 1) & ~((1ull << a) - 1);
@@ -63,37 +69,74 @@ __device__ __forceinline__ unsigned long long key_mask(unsigned long long v, int
   return m;
 }
 
+// The query tile of 32 pairs from x0 + r32: this lane's pair.
+struct Pair {
+  bool ok;
+  int row, hq;
+  unsigned long long vis;
+};
+__device__ __forceinline__ Pair pair_at(const Kv4Params& p, int hk, int x) {
+  Pair q;
+  q.ok = x < p.n_pairs;
+  q.row = q.ok ? x / p.g : 0;
+  q.hq = hk * p.g + (q.ok ? x - q.row * p.g : 0);
+  q.vis = q.ok && p.R > 0 ? p.vis[q.row / p.B] : 0;
+  return q;
+}
+// Lane blocks that some pair of [x0, x1) sees.
+__device__ __forceinline__ unsigned long long blocks_seen(const Kv4Params& p, int x0, int x1) {
+  unsigned long long v = 0;
+  if (p.R > 0 && x0 < p.n_pairs) {
+    const int l1 = (min(x1, p.n_pairs) - 1) / p.g / p.B;
+    for (int l = x0 / p.g / p.B; l <= l1; ++l) v |= p.vis[l];
+  }
+  return v;
+}
+// The first key tile at or after t, before t_end, that a workgroup with wg_vis sees.
+template <int KT>
+__device__ __forceinline__ int next_visible(const Kv4Params& p, unsigned long long wg_vis, int t, int t_end) {
+  for (; t < t_end && t >= p.n_pre; ++t) {
+    const int row0 = (t - p.n_pre) * KT;
+    const int j0 = row0 / p.B, j1 = (min(row0 + KT, p.R) - 1) / p.B;
+    const unsigned long long upto = j1 >= 63 ? ~0ull : (1ull << (j1 + 1)) - 1;
+    if (wg_vis & upto & ~((1ull << j0) - 1)) break;
+  }
+  return t;
+}
+
+// ---------------------------------------------------------------- tile kernel
+// Many query tiles: eight (or four) of them, a wavefront each, share the key tiles
+// of a workgroup.  While prefix tile i is worked on, tile i + 1 is complete in LDS,
+// tile i + 2 goes there from registers and tile i + 3 is loaded: each wavefront
+// multiplies K of tile i + 1 while the softmax of tile i runs between the MFMAs, then
+// V of tile i, with the conversion of tile i + 2 between the last of them.  Three
+// buffers, one barrier a tile.
 template <int D>
-__global__ __launch_bounds__(K4_THREADS) void lane_attn_kv4_kernel(Kv4Params p) {
+__global__ __launch_bounds__(K4_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void lane_attn_kv4_kernel(Kv4Params p) {
   constexpr int KS = D / 16;        // MFMA k-steps of S^T = K Q^T
   constexpr int DT = D / 32;        // 32-row tiles of O^T; scale blocks of a row
   constexpr int ROWB = 2 * D;       // bytes of a K or V row in LDS
   constexpr int TB = K4_KT * ROWB;
   constexpr int SEGS = D / 8;       // 16-byte segments of a row
   constexpr int NL = 2 * K4_KT * SEGS / K4_THREADS;   // bf16 segments per thread of a lane tile
-  __shared__ __attribute__((aligned(1024))) char lds[4 * TB];   // two buffers of K then V
+  constexpr int AHEAD = 4;          // K fragments read ahead
+  __shared__ __attribute__((aligned(1024))) char lds[6 * TB];   // three buffers of K then V
 
   const int hk = blockIdx.y, split = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r32 = lane & 31, hh = lane >> 5, lgrp = lane >> 4, lg = lane & 15;
-  const int x0 = blockIdx.x * 32 * K4_WAVES;
-  const int x = x0 + w * 32 + r32;
-  const bool ok = x < p.n_pairs;
-  const int row = ok ? x / p.g : 0;
-  const int hq = hk * p.g + (ok ? x - row * p.g : 0);
-  unsigned long long my_vis = 0, wg_vis = 0;
-  if (p.R > 0) {
-    if (ok) my_vis = p.vis[row / p.B];
-    const int l1 = (min(x0 + 32 * K4_WAVES, p.n_pairs) - 1) / p.g / p.B;
-    for (int l = x0 / p.g / p.B; l <= l1; ++l) wg_vis |= p.vis[l];
-  }
+  const int x0 = blockIdx.x * 32 * p.tpw;
+  const bool computing = w < p.tpw && x0 + w * 32 < p.n_pairs;
+  const Pair pr = pair_at(p, hk, w < p.tpw ? x0 + w * 32 + r32 : p.n_pairs);
+  const unsigned long long wg_vis = blocks_seen(p, x0, x0 + 32 * p.tpw);
 
   bf16x8 qf[KS];
   {
-    const uint16_t* qrow = p.q + ((size_t)row * p.Hq + hq) * D;
+    const uint16_t* qrow = p.q + ((size_t)pr.row * p.Hq + pr.hq) * D;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = ok ? load_bf16x8(qrow + ks * 16 + hh * 8) : zero_bf16x8();
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = pr.ok ? load_bf16x8(qrow + ks * 16 + hh * 8) : zero_bf16x8();
   }
   f32x16 oacc[DT];
 #pragma unroll
@@ -102,18 +145,6 @@ __global__ __launch_bounds__(K4_THREADS) void lane_attn_kv4_kernel(Kv4Params p) 
     for (int r = 0; r < 16; ++r) oacc[dt][r] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
 
-  // The key tiles of this split that some pair of the workgroup sees.
-  const int t_end = (int)((long long)(split + 1) * p.n_tiles / p.n_split);
-  auto next_visible = [&](int t) {
-    for (; t < t_end && t >= p.n_pre; ++t) {
-      const int row0 = (t - p.n_pre) * K4_KT;
-      const int j0 = row0 / p.B, j1 = (min(row0 + K4_KT, p.R) - 1) / p.B;
-      const unsigned long long upto = j1 >= 63 ? ~0ull : (1ull << (j1 + 1)) - 1;
-      if (wg_vis & upto & ~((1ull << j0) - 1)) break;
-    }
-    return t;
-  };
-
   // Staging.  Row r's 16-byte segment s sits in slot s ^ f(r): f_K puts the 16 rows
   // that one LDS cycle of the K reads serves into different banks, f_V the rows of
   // a transpose read.
@@ -121,143 +152,259 @@ __global__ __launch_bounds__(K4_THREADS) void lane_attn_kv4_kernel(Kv4Params p) 
   auto fv = [](int r) {
     return D == 128 ? (4 * (r & 3)) ^ (2 * ((r >> 2) & 1)) : (4 * ((r >> 1) & 1)) ^ (2 * ((r >> 2) & 1));
   };
-  struct Stage {
-    i32x4 x[NL];      // lane tile: segments; prefix tile: x[0] the codes of 32 elements
+  struct Codes {      // of a prefix tile: this thread's 32 elements
+    i32x4 x;
     unsigned s;
   };
   constexpr int NP = 2 * K4_KT * DT;   // 16-byte pieces of codes of a tile (at D = 64 half the threads have none)
   const int prow = (tid & (NP / 2 - 1)) / DT, pblk = tid & (DT - 1), pv = tid / (NP / 2);
-  auto load_tile = [&](Stage& g, int t) {
-    if (t < p.n_pre) {
-      const int r = t * K4_KT + prow;
-      g.x[0] = i32x4{0, 0, 0, 0};
-      g.s = 0;
-      if (tid < NP && r < p.P) {
-        const size_t at = (((size_t)pv * p.Hkv + hk) * p.cap + r) * DT + pblk;
-        g.x[0] = reinterpret_cast<const i32x4*>(p.codes)[at];
-        g.s = p.scales[at];
-      }
-    } else {
-      const int r0 = (t - p.n_pre) * K4_KT;
-#pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        const int seg = tid + i * K4_THREADS;           // K rows, then V rows
-        const int sr = (seg / SEGS) % K4_KT, sv = seg / (SEGS * K4_KT);
-        const uint16_t* base = sv ? p.v_lane : p.k_lane;
-        g.x[i] = i32x4{0, 0, 0, 0};
-        if (r0 + sr < p.R)
-          g.x[i] = *reinterpret_cast<const i32x4*>(base + ((size_t)(r0 + sr) * p.Hkv + hk) * D + (seg % SEGS) * 8);
-      }
+  const bool stager = NP == K4_THREADS || tid < NP;
+  const size_t pat = (((size_t)(stager ? pv : 0) * p.Hkv + hk) * p.cap + prow) * DT + pblk;
+  auto load_codes = [&](Codes& g, int t) {   // (rows past the prefix are zero)
+    g.x = i32x4{0, 0, 0, 0};
+    g.s = 0;
+    if (stager && t * K4_KT + prow < p.P) {
+      const size_t at = pat + (size_t)t * (K4_KT * DT);
+      g.x = reinterpret_cast<const i32x4*>(p.codes)[at];
+      g.s = p.scales[at];
     }
   };
-  auto store_tile = [&](const Stage& g, int t, int buf) {
+  const int pdst = pv * TB + prow * ROWB, pf = pv ? fv(prow) : fk(prow);
+  auto store_piece = [&](const Codes& g, int buf, int j) {   // j = 0..3
+    *reinterpret_cast<bf16x8*>(lds + buf * 2 * TB + pdst + ((4 * pblk + j) ^ pf) * 16) =
+        mx4_bf16x8((unsigned)g.x[j], mx4_scale(g.s));
+  };
+  auto store_codes = [&](const Codes& g, int buf) {
+    if (stager) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) store_piece(g, buf, j);
+    }
+  };
+  auto load_rows = [&](i32x4 (&x)[NL], int t) {   // of lane tile t: K rows, then V rows
+    const int r0 = (t - p.n_pre) * K4_KT;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int seg = tid + i * K4_THREADS;
+      const int sr = (seg / SEGS) % K4_KT, sv = seg / (SEGS * K4_KT);
+      const uint16_t* base = sv ? p.v_lane : p.k_lane;
+      x[i] = i32x4{0, 0, 0, 0};
+      if (r0 + sr < p.R)
+        x[i] = *reinterpret_cast<const i32x4*>(base + ((size_t)(r0 + sr) * p.Hkv + hk) * D + (seg % SEGS) * 8);
+    }
+  };
+  auto store_rows = [&](const i32x4 (&x)[NL], int buf) {
     char* b = lds + buf * 2 * TB;
-    if (t < p.n_pre) {
-      if (tid < NP) {
-        const float sc = mx4_scale(g.s);
-        char* dst = b + pv * TB + prow * ROWB;
-        const int f = pv ? fv(prow) : fk(prow);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          *reinterpret_cast<bf16x8*>(dst + ((4 * pblk + j) ^ f) * 16) = mx4_bf16x8((unsigned)g.x[0][j], sc);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        const int seg = tid + i * K4_THREADS;
-        const int sr = (seg / SEGS) % K4_KT, sv = seg / (SEGS * K4_KT);
-        *reinterpret_cast<i32x4*>(b + sv * TB + sr * ROWB + ((seg % SEGS) ^ (sv ? fv(sr) : fk(sr))) * 16) = g.x[i];
-      }
+    for (int i = 0; i < NL; ++i) {
+      const int seg = tid + i * K4_THREADS;
+      const int sr = (seg / SEGS) % K4_KT, sv = seg / (SEGS * K4_KT);
+      *reinterpret_cast<i32x4*>(b + sv * TB + sr * ROWB + ((seg % SEGS) ^ (sv ? fv(sr) : fk(sr))) * 16) = x[i];
     }
   };
   const int ka = r32 * ROWB + ((hh ^ fk(r32)) * 16);   // K fragment (row r32, segment 2 ks + hh) at ka ^ 32 ks
   const int vr = 4 * hh + (lg >> 2);
   const int va = vr * ROWB + (((2 * (lgrp & 1) + ((lg & 3) >> 1)) ^ fv(vr)) * 16) + (lg & 1) * 8;
 
-  auto compute = [&](int t, int buf) {
-    const char* kt = lds + buf * 2 * TB;
-    unsigned long long km = ~0ull;
-    bool all = true;
-    if (t >= p.n_pre) {
-      km = key_mask(my_vis, (t - p.n_pre) * K4_KT, p.B, p.R);
-      if (!__ballot(km != 0)) return;
-      all = false;
-    } else if (p.P - t * K4_KT < K4_KT) {
-      km = (1ull << (p.P - t * K4_KT)) - 1;
-      all = false;
-    }
-    f32x16 s[2];
+  struct Scores {
+    f32x16 s[2];   // the two 32-key halves
+  };
+  auto kread = [&](int buf, int i) {
+    return *reinterpret_cast<const bf16x8*>(lds + buf * 2 * TB + (ka ^ (32 * (i >> 1))) + (i & 1) * 32 * ROWB);
+  };
+  auto vfrag = [&](int buf, int ks2, int dt) {
+    const uint16_t* a = reinterpret_cast<const uint16_t*>(lds + buf * 2 * TB + TB + (va ^ (64 * dt)) + 16 * ks2 * ROWB);
+    return cat_bf16x4(lds_read_tr16(a), lds_read_tr16(a + 8 * D));
+  };
+  const f32x16 zero16 = {};
+  auto qk = [&](Scores& sc, int buf) {
+#pragma unroll
+    for (int i = 0; i < 2 * KS; ++i)
+      sc.s[i & 1] = mfma32x32x16(kread(buf, i), qf[i >> 1], i < 2 ? zero16 : sc.s[i & 1]);
+  };
+  auto mask = [&](Scores& sc, unsigned long long km) {
+    const unsigned mw[2] = {(unsigned)km >> (4 * hh), (unsigned)(km >> 32) >> (4 * hh)};
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+      for (int r = 0; r < 16; ++r) sc.s[kb][r] = mw[kb] & (1u << (8 * (r >> 2) + (r & 3))) ? sc.s[kb][r] : -INFINITY;
+  };
+  auto max_piece = [&](float mx, const Scores& sc, int q) {   // q = 0..3: 8 scores
 #pragma unroll
-    for (int i = 0; i < 2 * KS; ++i) {
-      const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + (ka ^ (32 * (i >> 1))) + (i & 1) * 32 * ROWB);
-      s[i & 1] = mfma32x32x16(kf, qf[i >> 1], s[i & 1]);
-    }
-    if (!all) {
-      const unsigned mw[2] = {(unsigned)km >> (4 * hh), (unsigned)(km >> 32) >> (4 * hh)};
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[kb][r] = mw[kb] & (1u << (8 * (r >> 2) + (r & 3))) ? s[kb][r] : -INFINITY;
-    }
-    float mx = -INFINITY;
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
-    // (A pair that has seen no key yet keeps m_run = -inf, all of its P 0.)
-    const float m_new = fmaxf(m_run, pair_max32(mx) * p.scale_log2);
-    const float m_use = m_new == -INFINITY ? 0.f : m_new;
+    for (int r = 0; r < 8; ++r) mx = fmaxf(mx, sc.s[q >> 1][8 * (q & 1) + r]);
+    return mx;
+  };
+  // Returns the factor on O.  (A pair that has seen no key yet keeps m_run = -inf; its
+  // exponents are then taken from 0, all of its P are 0.)
+  auto new_max = [&](float mx, float& m_use) {
+    const float m_tile = pair_max32(mx) * p.scale_log2;
+    const float m_new = m_tile > m_run + K4_RESCALE_LOG2 ? m_tile : m_run;
+    m_use = m_new == -INFINITY ? 0.f : m_new;
     const float alpha = exp2_fast(m_run - m_use);
     m_run = m_new;
-    bf16x8 pk[4];
-    float rs = 0.f;
+    return alpha;
+  };
+  auto exp_pair = [&](const Scores& sc, bf16x8* pk, float m_use, float& rs, int q) {   // q = 0..15
+    const int ks2 = q >> 2, e = 2 * (q & 3), r = 8 * (ks2 & 1) + e;
+    const float p0 = exp2_fast(fmaf(sc.s[ks2 >> 1][r], p.scale_log2, -m_use));
+    const float p1 = exp2_fast(fmaf(sc.s[ks2 >> 1][r + 1], p.scale_log2, -m_use));
+    pk[ks2][e] = (__bf16)p0;
+    pk[ks2][e + 1] = (__bf16)p1;
+    rs += p0 + p1;
+  };
+  auto rescale = [&](float alpha) {   // (O only when some pair's reference has moved; otherwise alpha is 1)
+    if (__builtin_amdgcn_read_exec() & __ballot(alpha != 1.0f)) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+      for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float pe = exp2_fast(fmaf(s[q >> 1][8 * (q & 1) + e], p.scale_log2, -m_use));
-        rs += pe;
-        pk[q][e] = (__bf16)pe;
-      }
-    l_run = l_run * alpha + pair_sum32(rs);
+        for (int r = 0; r < 16; ++r) oacc[dt][r] *= alpha;
+    }
+  };
+  // O^T += V^T P^T, the second half of P's exponentials between the MFMAs of the
+  // first two steps and, where a prefix tile is to be stored, its pieces between
+  // those of the last two.  vf[0] holds the first step's fragments.
+  auto pv_product = [&](auto store_tag, const Scores& sc, bf16x8* pk, bf16x8 (*vf)[DT], float m_use, float alpha,
+                        float rs, int buf, const Codes& g, int sbuf) {   // (sbuf < 0: nothing to store)
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) oacc[dt][r] *= alpha;
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int ks2 = 0; ks2 < 4; ++ks2) {
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        const uint16_t* a = reinterpret_cast<const uint16_t*>(kt + TB + (va ^ (64 * dt)) + 16 * q * ROWB);
-        oacc[dt] = mfma32x32x16(cat_bf16x4(lds_read_tr16(a), lds_read_tr16(a + 8 * D)), pk[q], oacc[dt]);
+        if (ks2 < 3) vf[(ks2 + 1) & 1][dt] = vfrag(buf, ks2 + 1, dt);
+        oacc[dt] = mfma32x32x16(vf[ks2 & 1][dt], pk[ks2], oacc[dt]);
+        if (ks2 < 2) {
+#pragma unroll
+          for (int q = 0; q < 4 / DT; ++q) exp_pair(sc, pk, m_use, rs, 8 + ks2 * 4 + dt * (4 / DT) + q);
+        } else if (decltype(store_tag)::value && (dt & (DT / 2 - 1)) == 0) {
+          if (stager && sbuf >= 0) store_piece(g, sbuf, 2 * (ks2 - 2) + dt / (DT / 2));
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
+    }
+    l_run = l_run * alpha + pair_sum32(rs);
+  };
+  // Q K^T of the tile in buffer bq into nxt, with the max and the first half of the
+  // exponentials of cur between its MFMAs; then cur's P V.
+  auto hot_tile = [&](const Scores& cur, Scores& nxt, int bq, int bv, const Codes& g, int sbuf) {
+    bf16x8 kf[2 * KS], pk[4], vf[2][DT];
+    float mx = -INFINITY, m_use = 0.f, alpha = 1.f, rs = 0.f;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) kf[i] = kread(bq, i);
+    __builtin_amdgcn_sched_barrier(0);
+    constexpr int MX = KS / 2;                 // MFMAs with a piece of the max
+    constexpr int EX = 2 * KS - MX;            // and with exponentials
+#pragma unroll
+    for (int i = 0; i < 2 * KS; ++i) {
+      if (i + AHEAD < 2 * KS) kf[i + AHEAD] = kread(bq, i + AHEAD);
+      else if (i + DT >= 2 * KS) vf[0][i + DT - 2 * KS] = vfrag(bv, 0, i + DT - 2 * KS);
+      nxt.s[i & 1] = mfma32x32x16(kf[i], qf[i >> 1], i < 2 ? zero16 : nxt.s[i & 1]);
+      if (i < MX) {
+#pragma unroll
+        for (int q = 0; q < 4 / MX; ++q) mx = max_piece(mx, cur, i * (4 / MX) + q);
+        if (i == MX - 1) alpha = new_max(mx, m_use);
+      } else {
+        const int j = i - MX;
+#pragma unroll
+        for (int q = 8 * j / EX; q < 8 * (j + 1) / EX; ++q) {
+          exp_pair(cur, pk, m_use, rs, q);
+          // (Left alone, the compiler sinks these past the branch below to their use.)
+          const i32x4 pq = __builtin_bit_cast(i32x4, pk[q >> 2]);
+          asm volatile("" ::"v"(pq[q & 3]), "v"(rs));
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    rescale(alpha);
+    pv_product(IntTag<1>{}, cur, pk, vf, m_use, alpha, rs, bv, g, sbuf);
+  };
+  auto cold_tile = [&](const Scores& cur, int bv) {   // softmax and P V alone
+    bf16x8 pk[4], vf[2][DT];
+    float mx = -INFINITY, m_use, rs = 0.f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) mx = max_piece(mx, cur, q);
+    const float alpha = new_max(mx, m_use);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) exp_pair(cur, pk, m_use, rs, q);
+    rescale(alpha);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) vf[0][dt] = vfrag(bv, 0, dt);
+    __builtin_amdgcn_sched_barrier(0);
+    pv_product(IntTag<0>{}, cur, pk, vf, m_use, alpha, rs, bv, Codes{}, -1);
   };
 
-  int t = next_visible((int)((long long)split * p.n_tiles / p.n_split));
-  Stage g;
-  if (t < t_end) {
-    load_tile(g, t);
-    store_tile(g, t, 0);
+  // This split's tiles: prefix tiles [t0, pe), then the lane tiles that some pair of
+  // the workgroup sees.
+  const int t0 = (int)((long long)split * p.n_tiles / p.n_split);
+  const int t_end = (int)((long long)(split + 1) * p.n_tiles / p.n_split);
+  const int pe = min(t_end, p.n_pre);
+  i32x4 rows[NL];
+  const int lt0 = next_visible<K4_KT>(p, wg_vis, max(p.n_pre, t0), t_end);   // first lane tile
+  if (t0 < pe) {
+    auto third = [](int x) { return x >= 3 ? x - 3 : x; };
+    Codes g;
+    load_codes(g, t0);
+    store_codes(g, 0);
+    if (t0 + 1 < pe) {
+      load_codes(g, t0 + 1);
+      store_codes(g, 1);
+    }
+    if (t0 + 2 < pe) load_codes(g, t0 + 2);
+    __syncthreads();
+    Scores sa, sb;
+    if (computing) qk(sa, 0);
+    int t = t0, buf = 0;
+    auto step = [&](Scores& cur, Scores& nxt) {   // t + 1 < pe
+      const int sbuf = t + 2 < pe ? third(buf + 2) : -1;
+      if (computing) hot_tile(cur, nxt, third(buf + 1), buf, g, sbuf);
+      else if (sbuf >= 0) store_codes(g, sbuf);
+      if (t + 3 < pe) load_codes(g, t + 3);
+      // (__syncthreads would wait for the loads too)
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      ++t;
+      buf = third(buf + 1);
+    };
+    auto last = [&](Scores& cur) {
+      if (computing) {
+        if (p.P - t * K4_KT < K4_KT) mask(cur, (1ull << (p.P - t * K4_KT)) - 1);
+        cold_tile(cur, buf);
+      }
+    };
+    while (t + 2 < pe) {   // (two at a time: the scores keep their registers)
+      step(sa, sb);
+      step(sb, sa);
+    }
+    if (t + 1 < pe) {
+      step(sa, sb);
+      if (lt0 < t_end) load_rows(rows, lt0);
+      last(sb);
+    } else {
+      if (lt0 < t_end) load_rows(rows, lt0);
+      last(sa);
+    }
+    __syncthreads();
+  } else if (lt0 < t_end) {
+    load_rows(rows, lt0);
   }
-  int tn = next_visible(t + 1);
-  if (tn < t_end) load_tile(g, tn);
+  // Lane tiles, one after another in two buffers.
+  if (lt0 < t_end) store_rows(rows, 0);
   __syncthreads();
-  for (int buf = 0; t < t_end; buf ^= 1) {
-    if (tn < t_end) store_tile(g, tn, buf ^ 1);
-    const int t2 = next_visible(tn + 1);
-    if (t2 < t_end) load_tile(g, t2);
-    compute(t, buf);
+  for (int t = lt0, buf = 0; t < t_end; buf ^= 1) {
+    const int tn = next_visible<K4_KT>(p, wg_vis, t + 1, t_end);
+    if (tn < t_end) load_rows(rows, tn);
+    if (computing) {
+      const unsigned long long km = key_mask<K4_KT>(pr.vis, (t - p.n_pre) * K4_KT, p.B, p.R);
+      if (__ballot(km != 0)) {
+        Scores sc;
+        qk(sc, buf);
+        mask(sc, km);
+        cold_tile(sc, buf);
+      }
+    }
+    if (tn < t_end) store_rows(rows, buf ^ 1);
     __syncthreads();
     t = tn;
-    tn = t2;
   }
 
-  if (!ok) return;
-  const size_t orow = (size_t)row * p.Hq + hq;
+  if (!computing || !pr.ok) return;
+  const size_t orow = (size_t)pr.row * p.Hq + pr.hq;
   if (p.n_split == 1) {
     const float inv_l = 1.0f / l_run;
     uint16_t* op = p.o + orow * D;
@@ -289,25 +436,261 @@ __global__ __launch_bounds__(K4_THREADS) void lane_attn_kv4_kernel(Kv4Params p) 
   }
 }
 
-// Combines the key splits of each (row, head): D / 4 lanes each, 4 elements a lane,
-// in ascending order of the splits.
+// ---------------------------------------------------------------- unit kernel
+// Few query tiles: a workgroup serves one, and its eight wavefronts share out the
+// keys in units of 32, each with a softmax state of its own (combined in LDS at the
+// end), so the loop has no barrier.  K needs no LDS: lane (key, half) of a wavefront
+// takes the 16 bytes of a scale block, converts them and has its operand of four
+// MFMA steps (q's fragments follow the same order of d).  V is converted into an LDS
+// region of the wavefront's own for the transpose reads.
 template <int D>
+__global__ __launch_bounds__(K4_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void lane_attn_kv4_unit_kernel(Kv4Params p) {
+  constexpr int KS = D / 16, DT = D / 32, DC = D / 64;
+  constexpr int VROW = D + 32;              // elements of a V row in LDS
+  constexpr int WBUF = K4_UT * VROW;        // of a wavefront
+  constexpr int OSTR = D + 4;               // fp32 per row of the merge area
+  constexpr int LDSB = K4_WAVES * 32 * (OSTR + 2) * 4 > K4_WAVES * WBUF * 2 ? K4_WAVES * 32 * (OSTR + 2) * 4
+                                                                           : K4_WAVES * WBUF * 2;
+  __shared__ __attribute__((aligned(16))) char lds[LDSB];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r32 = lane & 31, hh = lane >> 5, lgrp = lane >> 4, lg = lane & 15;
+  const int hk = blockIdx.x % p.Hkv, x0 = (int)(blockIdx.x / p.Hkv) * 32, split = blockIdx.z;
+  uint16_t* v_s = reinterpret_cast<uint16_t*>(lds) + w * WBUF;
+  const Pair pr = pair_at(p, hk, x0 + r32);
+  const unsigned long long wg_vis = blocks_seen(p, x0, x0 + 32);
+
+  // q's fragment c, j: elements 64 c + 32 hh + 8 j + (0..7).
+  bf16x8 qf[KS];
+  {
+    const uint16_t* qrow = p.q + ((size_t)pr.row * p.Hq + pr.hq) * D + 32 * hh;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) qf[i] = pr.ok ? load_bf16x8(qrow + 64 * (i >> 2) + 8 * (i & 3)) : zero_bf16x8();
+  }
+  f32x16 oacc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[dt][r] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+
+  struct Codes {
+    i32x4 x[2 * DC];   // of K, then of V: block 2 c + hh of the key's row
+    unsigned ks, vs;   // scale bytes of the rows
+  };
+  const size_t vplane = (size_t)p.Hkv * p.cap;
+  auto load_codes = [&](Codes& g, int u) {
+    const int key = min(u * K4_UT + r32, p.P - 1);   // (a key past the prefix repeats the last one, with P = 0)
+    const size_t row = (size_t)hk * p.cap + key;
+    const i32x4* kc = reinterpret_cast<const i32x4*>(p.codes) + row * DT + hh;
+    const i32x4* vc = kc + vplane * DT;
+#pragma unroll
+    for (int c = 0; c < DC; ++c) {
+      g.x[c] = kc[2 * c];
+      g.x[DC + c] = vc[2 * c];
+    }
+    if (DT == 4) {
+      g.ks = reinterpret_cast<const unsigned*>(p.scales)[row];
+      g.vs = reinterpret_cast<const unsigned*>(p.scales)[vplane + row];
+    } else {
+      g.ks = reinterpret_cast<const uint16_t*>(p.scales)[row];
+      g.vs = reinterpret_cast<const uint16_t*>(p.scales)[vplane + row];
+    }
+  };
+  // A unit: K's and V's operands of this lane's key, the keys its pair sees.
+  auto compute = [&](const bf16x8 (&kf)[KS], const bf16x8 (&vf)[KS], unsigned km) {
+    // The region is this wavefront's own: its LDS operations complete in issue
+    // order; the fences order the compiler alone.
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+      *reinterpret_cast<bf16x8*>(&v_s[r32 * VROW + 64 * (i >> 2) + 32 * hh + 8 * (i & 3)]) = vf[i];
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    f32x16 s = {}, s1 = {};
+#pragma unroll
+    for (int i = 0; i < KS; i += 2) {
+      s = mfma32x32x16(kf[i], qf[i], s);
+      s1 = mfma32x32x16(kf[i + 1], qf[i + 1], s1);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] += s1[r];
+    if (__ballot(km != ~0u)) {
+      const unsigned mw = km >> (4 * hh);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = mw & (1u << (8 * (r >> 2) + (r & 3))) ? s[r] : -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
+    const float m_tile = pair_max32(mx) * p.scale_log2;
+    const float m_new = m_tile > m_run + K4_RESCALE_LOG2 ? m_tile : m_run;
+    const float m_use = m_new == -INFINITY ? 0.f : m_new;   // (no key seen yet: all P are 0)
+    const float alpha = exp2_fast(m_run - m_use);
+    m_run = m_new;
+    float rs = 0.f;
+    bf16x8 pk[2];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float pe = exp2_fast(fmaf(s[r], p.scale_log2, -m_use));
+      rs += pe;
+      pk[r >> 3][r & 7] = (__bf16)pe;
+    }
+    l_run = l_run * alpha + pair_sum32(rs);
+    if (__ballot(alpha != 1.0f)) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[dt][r] *= alpha;
+    }
+#pragma unroll
+    for (int ks2 = 0; ks2 < 2; ++ks2)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const uint16_t* va = &v_s[(16 * ks2 + 4 * hh + (lg >> 2)) * VROW + dt * 32 + 16 * (lgrp & 1) + 4 * (lg & 3)];
+        oacc[dt] = mfma32x32x16(cat_bf16x4(lds_read_tr16(va), lds_read_tr16(va + 8 * VROW)), pk[ks2], oacc[dt]);
+      }
+  };
+
+  // Wavefront w takes every eighth unit of the split's share, the next prefix unit's
+  // loads in flight.
+  const int u0 = (int)((long long)split * p.n_tiles / p.n_split);
+  const int u_end = (int)((long long)(split + 1) * p.n_tiles / p.n_split);
+  auto seen = [&](int u) {   // this unit or a later one of the wavefront that the tile sees
+    for (; u < u_end && u >= p.n_pre; u += K4_WAVES) {
+      const int row0 = (u - p.n_pre) * K4_UT;
+      const int j0 = row0 / p.B, j1 = (min(row0 + K4_UT, p.R) - 1) / p.B;
+      const unsigned long long upto = j1 >= 63 ? ~0ull : (1ull << (j1 + 1)) - 1;
+      if (wg_vis & upto & ~((1ull << j0) - 1)) break;
+    }
+    return u;
+  };
+  int u = u0 + w;
+  {
+    Codes g;
+    const int pe = min(u_end, p.n_pre);
+    if (u < pe) load_codes(g, u);
+    while (u < pe) {
+      bf16x8 kf[KS], vf[KS];
+#pragma unroll
+      for (int c = 0; c < DC; ++c) {
+        const float ksc = mx4_scale((g.ks >> (16 * c + 8 * hh)) & 255), vsc = mx4_scale((g.vs >> (16 * c + 8 * hh)) & 255);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          kf[4 * c + j] = mx4_bf16x8((unsigned)g.x[c][j], ksc);
+          vf[4 * c + j] = mx4_bf16x8((unsigned)g.x[DC + c][j], vsc);
+        }
+      }
+      const int left = p.P - u * K4_UT;
+      u += K4_WAVES;
+      if (u < pe) load_codes(g, u);
+      compute(kf, vf, left < K4_UT ? (1u << left) - 1 : ~0u);
+    }
+  }
+  for (u = seen(u); u < u_end; u = seen(u + K4_WAVES)) {
+    const int r = min((u - p.n_pre) * K4_UT + r32, p.R - 1);
+    const size_t at = ((size_t)r * p.Hkv + hk) * D + 32 * hh;
+    bf16x8 kf[KS], vf[KS];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      kf[i] = load_bf16x8(p.k_lane + at + 64 * (i >> 2) + 8 * (i & 3));
+      vf[i] = load_bf16x8(p.v_lane + at + 64 * (i >> 2) + 8 * (i & 3));
+    }
+    compute(kf, vf, (unsigned)key_mask<K4_UT>(pr.vis, (u - p.n_pre) * K4_UT, p.B, p.R));
+  }
+
+  // Combine the wavefronts' states, in ascending order.
+  __syncthreads();
+  float* o_s = reinterpret_cast<float*>(lds);
+  float* ml_s = o_s + K4_WAVES * 32 * OSTR;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int rg = 0; rg < 4; ++rg)
+      *reinterpret_cast<float4*>(&o_s[(w * 32 + r32) * OSTR + dt * 32 + 8 * rg + 4 * hh]) =
+          make_float4(oacc[dt][rg * 4 + 0], oacc[dt][rg * 4 + 1], oacc[dt][rg * 4 + 2], oacc[dt][rg * 4 + 3]);
+  if (hh == 0) {
+    ml_s[(w * 32 + r32) * 2 + 0] = m_run;
+    ml_s[(w * 32 + r32) * 2 + 1] = l_run;
+  }
+  __syncthreads();
+  constexpr int TPR = D / 8;                  // threads per pair
+  constexpr int RPP = K4_THREADS / TPR;       // pairs per pass
+  const int d0 = (tid % TPR) * 8;
+  for (int r = tid / TPR; r < 32 && x0 + r < p.n_pairs; r += RPP) {
+    float mw[K4_WAVES], M = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < K4_WAVES; ++i) {
+      mw[i] = ml_s[(i * 32 + r) * 2];
+      M = fmaxf(M, mw[i]);
+    }
+    float L = 0.f, acc[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < K4_WAVES; ++i) {
+      const float wgt = mw[i] == -INFINITY ? 0.f : exp2_fast(mw[i] - M);
+      L += ml_s[(i * 32 + r) * 2 + 1] * wgt;
+      const f32x4 a = *reinterpret_cast<const f32x4*>(&o_s[(i * 32 + r) * OSTR + d0]);
+      const f32x4 b = *reinterpret_cast<const f32x4*>(&o_s[(i * 32 + r) * OSTR + d0 + 4]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc[e] += a[e] * wgt;
+        acc[4 + e] += b[e] * wgt;
+      }
+    }
+    const int row = (x0 + r) / p.g;
+    const size_t orow = (size_t)row * p.Hq + hk * p.g + (x0 + r - row * p.g);
+    if (p.n_split == 1) {
+      const float inv = 1.0f / L;
+      bf16x8 out;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) out[e] = (__bf16)(acc[e] * inv);
+      *reinterpret_cast<bf16x8*>(p.o + orow * D + d0) = out;
+      if (p.lse && d0 == 0) p.lse[orow] = (M + log2f(L)) * K4_LN2;
+    } else {
+      const size_t at = (size_t)split * p.n_rows * p.Hq + orow;
+      *reinterpret_cast<f32x4*>(p.part_o + at * D + d0) = f32x4{acc[0], acc[1], acc[2], acc[3]};
+      *reinterpret_cast<f32x4*>(p.part_o + at * D + d0 + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
+      if (d0 == 0) {
+        p.part_ml[at * 2] = M;
+        p.part_ml[at * 2 + 1] = L;
+      }
+    }
+  }
+}
+
+// Combines the NS key splits of each (row, head): D / 4 lanes each, 4 elements a
+// lane, every split's loads issued at once, summed in ascending order.
+template <int D, int NS>
 __global__ __launch_bounds__(256) void kv4_merge_kernel(const float* part_o, const float* part_ml, int n_rowheads,
-                                                        int n_split, uint16_t* o, float* lse) {
+                                                        uint16_t* o, float* lse) {
   constexpr int LPR = D / 4;
   const int rh = blockIdx.x * (256 / LPR) + threadIdx.x / LPR, sl = threadIdx.x % LPR;
   if (rh >= n_rowheads) return;
+  float m[NS], l[NS];
+  f32x4 v[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    const float2 ml = *reinterpret_cast<const float2*>(part_ml + ((size_t)s * n_rowheads + rh) * 2);
+    m[s] = ml.x;
+    l[s] = ml.y;
+    v[s] = *reinterpret_cast<const f32x4*>(part_o + ((size_t)s * n_rowheads + rh) * D + sl * 4);
+  }
   float M = -INFINITY;
-  for (int s = 0; s < n_split; ++s) M = fmaxf(M, part_ml[((size_t)s * n_rowheads + rh) * 2]);
+#pragma unroll
+  for (int s = 0; s < NS; ++s) M = fmaxf(M, m[s]);
   float L = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < n_split; ++s) {
-    const float2 ml = *reinterpret_cast<const float2*>(part_ml + ((size_t)s * n_rowheads + rh) * 2);
-    const float wgt = exp2_fast(ml.x - M);   // (0 where the split saw no key)
-    L += ml.y * wgt;
-    const f32x4 v = *reinterpret_cast<const f32x4*>(part_o + ((size_t)s * n_rowheads + rh) * D + sl * 4);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] += v[e] * wgt;
+  for (int s = 0; s < NS; ++s) {
+    const float wgt = exp2_fast(m[s] - M);   // (0 where the split saw no key; M is finite)
+    L += l[s] * wgt;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += v[s][e] * wgt;
   }
   const float inv = 1.0f / L;
   bf16x4 out;
@@ -318,8 +701,10 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(const float* part_o, con
 }
 
 // ------------------------------------------------------------------ host
+constexpr int K4_MAX_SPLIT = 32;
 struct Kv4Pass {
-  int n_rows, n_pairs, q_wgs, n_pre, n_tiles, n_split;
+  bool units;        // unit kernel (else the tile kernel)
+  int n_rows, n_pairs, n_pre, n_tiles, n_split, tpw;
   size_t ws;
 };
 
@@ -328,11 +713,21 @@ static Kv4Pass kv4_pass(int n_rows, int R, int P, int Hq, int Hkv, int D) {
   Kv4Pass s{};
   s.n_rows = n_rows;
   s.n_pairs = n_rows * (Hq / Hkv);
-  s.q_wgs = (s.n_pairs + 32 * K4_WAVES - 1) / (32 * K4_WAVES);
-  s.n_pre = (P + K4_KT - 1) / K4_KT;
-  s.n_tiles = s.n_pre + (R + K4_KT - 1) / K4_KT;
+  const long long q_tiles = (s.n_pairs + 31) / 32;
+  const int units = (P + K4_UT - 1) / K4_UT + (R + K4_UT - 1) / K4_UT;
   s.n_split = 1;
-  while (s.n_split < 64 && (long long)s.q_wgs * Hkv * s.n_split < 256 && s.n_tiles >= 4 * s.n_split) s.n_split *= 2;
+  s.units = q_tiles * Hkv <= 256;
+  if (s.units) {
+    s.n_pre = (P + K4_UT - 1) / K4_UT;
+    s.n_tiles = units;
+    while (s.n_split < K4_MAX_SPLIT && q_tiles * Hkv * s.n_split * 2 <= 256 && units >= 4 * K4_WAVES * s.n_split) s.n_split *= 2;
+  } else {
+    s.n_pre = (P + K4_KT - 1) / K4_KT;
+    s.n_tiles = s.n_pre + (R + K4_KT - 1) / K4_KT;
+    s.tpw = K4_WAVES;
+    const long long wgs = (q_tiles + s.tpw - 1) / s.tpw * Hkv;
+    while (s.n_split < 16 && wgs * s.n_split < 256 && s.n_tiles >= 6 * s.n_split) s.n_split *= 2;
+  }
   s.ws = s.n_split > 1 ? (size_t)s.n_split * n_rows * Hq * (D + 2) * sizeof(float) : 0;
   return s;
 }
@@ -350,14 +745,29 @@ static hipError_t run_kv4_pass(Kv4Params p, const Kv4Pass& s, void* ws, hipStrea
   p.n_pre = s.n_pre;
   p.n_tiles = s.n_tiles;
   p.n_split = s.n_split;
+  p.tpw = s.tpw;
   p.part_o = static_cast<float*>(ws);
   p.part_ml = p.part_o + (size_t)s.n_split * s.n_rows * p.Hq * D;
-  hipLaunchKernelGGL(lane_attn_kv4_kernel<D>, dim3(s.q_wgs, p.Hkv, s.n_split), dim3(K4_THREADS), 0, stream, p);
+  const int q_tiles = (s.n_pairs + 31) / 32;
+  if (s.units)
+    hipLaunchKernelGGL(lane_attn_kv4_unit_kernel<D>, dim3((unsigned)(q_tiles * p.Hkv), 1, s.n_split), dim3(K4_THREADS), 0,
+                       stream, p);
+  else
+    hipLaunchKernelGGL(lane_attn_kv4_kernel<D>, dim3((q_tiles + s.tpw - 1) / s.tpw, p.Hkv, s.n_split), dim3(K4_THREADS),
+                       0, stream, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || s.n_split == 1) return e;
   const int nrh = s.n_rows * p.Hq, per = 256 / (D / 4);
-  hipLaunchKernelGGL(kv4_merge_kernel<D>, dim3((nrh + per - 1) / per), dim3(256), 0, stream, p.part_o, p.part_ml, nrh,
-                     s.n_split, p.o, p.lse);
+  const dim3 grid((nrh + per - 1) / per);
+#define AL_K4_MERGE(NS)                                                                                    \
+  case NS:                                                                                                 \
+    hipLaunchKernelGGL((kv4_merge_kernel<D, NS>), grid, dim3(256), 0, stream, p.part_o, p.part_ml, nrh, p.o, p.lse); \
+    break;
+  switch (s.n_split) {
+    AL_K4_MERGE(2) AL_K4_MERGE(4) AL_K4_MERGE(8) AL_K4_MERGE(16) AL_K4_MERGE(32)
+    default: return hipErrorInvalidValue;
+  }
+#undef AL_K4_MERGE
   return hipGetLastError();
 }
 
