@@ -1,6 +1,6 @@
 """Binding of libasynclane.so (the C ABI in include/asynclane.h): ctypes, and a
 small CPython module (csrc/fast_call.cpp) that marshals the ordinary case of
-the three calls of a decode step natively (~16 us of Python per call before).
+the calls of a decode step natively (~16 us of Python per call before).
 
 Argument marshalling only: every step of the decode-step hot path runs in the
 library's HIP kernels.  PyTorch supplies device memory and the current HIP
@@ -95,7 +95,7 @@ class _NoFast:
     def attn(*args):
         return None
 
-    lmhead = select = attn
+    lmhead = select = lmhead_mx4 = attn_kv4 = quantize = dequantize = store = attn
 
 
 def _load_fast(lib):
@@ -619,6 +619,9 @@ def mx4_quantize(x, codes=None, scales=None):
     [..., n/2] and one scale byte per 32 elements [..., n/32], both uint8.
     Returns (codes, scales)."""
     lib = _lib or library()
+    r = _fast.quantize(x, codes, scales)
+    if r is not None:
+        return r
     _tensor(x, "x", torch.bfloat16)
     if x.dim() < 1:
         raise AsyncLaneError(f"x: [..., n] expected, got shape {tuple(x.shape)}")
@@ -640,6 +643,9 @@ def mx4_dequantize(codes, scales, y=None):
     [..., n/32] (uint8) to y [..., n].  A whole prefix cache of kv4_store is such
     a pair."""
     lib = _lib or library()
+    r = _fast.dequantize(codes, scales, y)
+    if r is not None:
+        return r
     lead, n = _mx4_pair(codes, scales)
     if y is None:
         y = torch.empty(lead + (n,), dtype=torch.bfloat16, device=codes.device)
@@ -667,6 +673,8 @@ def kv4_store(k, v, kv_codes, kv_scales, row_idx=None, start=0):
     [2][Hkv][cap][D/2], kv_scales [2][Hkv][cap][D/32] (uint8, written in place).
     A row whose index lies outside [0, cap) is left out."""
     lib = _lib or library()
+    if _fast.store(k, v, kv_codes, kv_scales, row_idx, start):
+        return
     Hkv, cap, D = _kv4_cache(kv_codes, kv_scales)
     _tensor(k, "k", torch.bfloat16)
     if k.dim() != 3 or tuple(k.shape[1:]) != (Hkv, D):
@@ -693,6 +701,10 @@ def lane_attn_forward_kv4(q, k_lane, v_lane, kv_codes, kv_scales, P, parent, B, 
     from 1.  Refresh rows are quantised into the cache in place first.  Returns
     (o, lse, o_ref, lse_ref)."""
     lib = _lib or library()
+    r = _fast.attn_kv4(q, k_lane, v_lane, kv_codes, kv_scales, P, parent, B, scale, refresh_idx, q_ref,
+                       k_ref, v_ref, o, lse, o_ref, lse_ref, want_lse, workspace)
+    if r is not None:
+        return r
     bf16, f32 = torch.bfloat16, torch.float32
     Hkv, cap, D = _kv4_cache(kv_codes, kv_scales)
     P, L = int(P), len(parent)
@@ -789,6 +801,10 @@ def lmhead_confidence_mx4(hidden, W_mx4, V, row_idx=None, suppress_eos=None, eos
     of a [V][d] weight, d hidden's width (a multiple of 32).  Returns (conf,
     argmax, lse)."""
     lib = _lib or library()
+    r = _fast.lmhead_mx4(hidden, W_mx4, V, row_idx, suppress_eos, eos_id, conf, argmax, lse, want_lse,
+                         workspace)
+    if r is not None:
+        return r
     V = int(V)
     n_rows, d, V, N, conf, argmax, lse = _lmhead_args(hidden, W_mx4, row_idx, suppress_eos, conf,
                                                       argmax, lse, want_lse, V=V, mx4=True)

@@ -1,5 +1,5 @@
-// CPython entry points of the three calls of a decode step: the argument
-// marshalling of _lib.py in native code for the ordinary case.
+// CPython entry points of the calls of a decode step (the 4-bit ones too): the
+// argument marshalling of _lib.py in native code for the ordinary case.
 //
 // What bounds a small call is the host: checking 14 tensors, allocating the
 // outputs and a 25-argument ctypes call took ~16 us in Python (attention and
@@ -17,6 +17,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <vector>
 
 #include "../../include/asynclane.h"
 
@@ -30,6 +31,14 @@ decltype(&::lmhead_packed_weight_size) f_lm_packed_size;
 decltype(&::lmhead_confidence) f_lm;
 decltype(&::lmhead_confidence_packed) f_lm_packed;
 decltype(&::select_unmask) f_select;
+decltype(&::mx4_quantize) f_quantize;
+decltype(&::mx4_dequantize) f_dequantize;
+decltype(&::kv4_store) f_store;
+decltype(&::lane_attn_kv4_workspace_size) f_attn_kv4_ws;
+decltype(&::lane_attn_forward_kv4) f_attn_kv4;
+decltype(&::lmhead_packed_weight_mx4_size) f_lm_mx4_size;
+decltype(&::lmhead_confidence_mx4_workspace_size) f_lm_mx4_ws;
+decltype(&::lmhead_confidence_mx4) f_lm_mx4;
 PyObject *py_check, *py_workspace, *py_raw_stream;   // _check, _workspace, current raw stream
 
 // Arguments as the library takes them.  What is not exactly that clears ok: the
@@ -305,9 +314,11 @@ PyObject* attn(PyObject*, PyObject* const* a, Py_ssize_t na) {
 
 // lmhead(hidden, W, V or None, row_idx, suppress_eos, eos_id, conf, argmax,
 //        lse, want_lse, workspace): V given = W is the packed copy.
+// lmhead_mx4: the same with W the packed 4-bit copy, V given.
+template <bool MX4>
 PyObject* lmhead(PyObject*, PyObject* const* a, Py_ssize_t na) {
   return guarded([&](PyObject** keep) -> PyObject* {
-    if (na != 11) return decline();
+    if (na != 11 || (MX4 && a[2] == Py_None)) return decline();
     Args g;
     const at::Tensor *h = g.tensor(a[0]), *W = g.tensor(a[1]), *ri = g.tensor(a[3]), *sup = g.tensor(a[4]),
                      *conf = g.tensor(a[6]), *arg = g.tensor(a[7]), *lse = g.tensor(a[8]);
@@ -319,8 +330,8 @@ PyObject* lmhead(PyObject*, PyObject* const* a, Py_ssize_t na) {
     int64_t V;
     if (packed) {
       V = g.to_int(a[2]);
-      const size_t nb = g.ok ? f_lm_packed_size((int)d, (int)V) : 0;
-      if (nb == 0 || W->numel() < (int64_t)(nb / 2)) return decline();
+      const size_t nb = g.ok ? (MX4 ? f_lm_mx4_size : f_lm_packed_size)((int)d, (int)V) : 0;
+      if (nb == 0 || W->numel() < (int64_t)(MX4 ? nb : nb / 2)) return decline();
     } else {
       if (W->dim() != 2 || W->size(1) != d || W->size(0) > INT32_MAX) return decline();
       V = W->size(0);
@@ -333,7 +344,7 @@ PyObject* lmhead(PyObject*, PyObject* const* a, Py_ssize_t na) {
     if (N == 0 || N > INT32_MAX) return decline();
     const int dev = current_device();
     void* hp = g.data(h, at::kBFloat16, dev);
-    void* Wp = g.data(W, at::kBFloat16, dev);
+    void* Wp = g.data(W, MX4 ? at::kByte : at::kBFloat16, dev);
     void* rp = g.data(ri, at::kInt, dev);
     void* sp = g.data_n(sup, at::kByte, dev, N);
     void* cp = g.data_n(conf, at::kFloat, dev, N);
@@ -342,7 +353,8 @@ PyObject* lmhead(PyObject*, PyObject* const* a, Py_ssize_t na) {
     if (!g.ok) return decline();
     void* stream = g.stream_of(dev);
     size_t bytes = 0;
-    void* ws = g.ok ? workspace(g, a[10], "lmhead", f_lm_ws((int)N, (int)d, (int)V), *h, dev, stream, &bytes, keep) : nullptr;
+    const size_t need = (MX4 ? f_lm_mx4_ws : f_lm_ws)((int)N, (int)d, (int)V);
+    void* ws = g.ok ? workspace(g, a[10], MX4 ? "lmhead_mx4" : "lmhead", need, *h, dev, stream, &bytes, keep) : nullptr;
     if (!g.ok) return decline();
     at::Tensor mc, ma, ml;
     const auto f32 = h->options().dtype(at::kFloat);
@@ -360,16 +372,243 @@ PyObject* lmhead(PyObject*, PyObject* const* a, Py_ssize_t na) {
     }
     int st;
     Py_BEGIN_ALLOW_THREADS
-    st = (packed ? f_lm_packed : f_lm)((al_bf16*)hp, (int)n_rows, (int32_t*)rp, (int)N, (al_bf16*)Wp, (int)d, (int)V,
-                                       (uint8_t*)sp, eos, (float*)cp, (int32_t*)ap, (float*)lp, ws, bytes, stream);
+    if (MX4)
+      st = f_lm_mx4((al_bf16*)hp, (int)n_rows, (int32_t*)rp, (int)N, (uint8_t*)Wp, (int)d, (int)V, (uint8_t*)sp, eos,
+                    (float*)cp, (int32_t*)ap, (float*)lp, ws, bytes, stream);
+    else
+      st = (packed ? f_lm_packed : f_lm)((al_bf16*)hp, (int)n_rows, (int32_t*)rp, (int)N, (al_bf16*)Wp, (int)d, (int)V,
+                                         (uint8_t*)sp, eos, (float*)cp, (int32_t*)ap, (float*)lp, ws, bytes, stream);
     Py_END_ALLOW_THREADS
-    if (!status_ok(st, packed ? "lmhead_confidence_packed" : "lmhead_confidence")) return nullptr;
+    if (!status_ok(st, MX4 ? "lmhead_confidence_mx4" : packed ? "lmhead_confidence_packed" : "lmhead_confidence"))
+      return nullptr;
     PyObject* t = PyTuple_New(3);
     if (!t) return nullptr;
     PyTuple_SET_ITEM(t, 0, wrap(conf, a[6], mc));
     PyTuple_SET_ITEM(t, 1, wrap(arg, a[7], ma));
     PyTuple_SET_ITEM(t, 2, wrap(lse, a[8], ml));
     return t;
+  });
+}
+
+// A 4-bit cache: kv_codes [2][Hkv][cap][D/2], kv_scales [2][Hkv][cap][D/32].
+struct Cache {
+  void *codes, *scales;
+  int64_t Hkv, cap, D;
+};
+Cache cache_of(Args& g, const at::Tensor* c, const at::Tensor* s, int dev) {
+  Cache k{};
+  if (!c || !s || c->dim() != 4 || s->dim() != 4 || c->size(0) != 2 || s->size(0) != 2) return g.no(k);
+  k.Hkv = c->size(1);
+  k.cap = c->size(2);
+  k.D = 2 * c->size(3);
+  if (s->size(1) != k.Hkv || s->size(2) != k.cap || s->size(3) != k.D / 32 || k.Hkv > INT32_MAX || k.cap > INT32_MAX ||
+      k.D > INT32_MAX)
+    return g.no(k);
+  k.codes = g.data(c, at::kByte, dev);
+  k.scales = g.data(s, at::kByte, dev);
+  return k;
+}
+
+// attn_kv4(q, k_lane, v_lane, kv_codes, kv_scales, P, parent, B, scale,
+//          refresh_idx, q_ref, k_ref, v_ref, o, lse, o_ref, lse_ref, want_lse,
+//          workspace)
+PyObject* attn_kv4(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  return guarded([&](PyObject** keep) -> PyObject* {
+    if (na != 19) return decline();
+    const auto bf16 = at::kBFloat16, f32 = at::kFloat;
+    Args g;
+    const at::Tensor *q = g.tensor(a[0]), *kl = g.tensor(a[1]), *vl = g.tensor(a[2]), *kc = g.tensor(a[3]),
+                     *ks = g.tensor(a[4]), *ri = g.tensor(a[9]), *qr = g.tensor(a[10]), *kr = g.tensor(a[11]),
+                     *vr = g.tensor(a[12]), *o = g.tensor(a[13]), *lse = g.tensor(a[14]), *o_r = g.tensor(a[15]),
+                     *lse_r = g.tensor(a[16]);
+    const bool want = g.to_bool(a[17]);
+    const float scale = g.to_float(a[8]);
+    const int P = g.to_int(a[5]);
+    if (!g.ok) return decline();
+    int32_t parent[AL_MAX_LANES];
+    const Py_ssize_t L = PyObject_Length(a[6]);
+    if (L < 0) PyErr_Clear();
+    if (L < 0 || L > AL_MAX_LANES) return decline();
+    g.host_array(a[6], parent, L);
+    if (!g.ok) return decline();
+    const int dev = current_device();
+    const Cache kv = cache_of(g, kc, ks, dev);
+    if (!g.ok || P < 0 || P > kv.cap) return decline();
+    int64_t n_ref = 0, Hq = 0;
+    int B = 1;
+    void *qp = nullptr, *klp = nullptr, *vlp = nullptr;
+    at::Tensor mo, ml, mor, mlr;
+    void *op = nullptr, *lp = nullptr, *orp = nullptr, *lrp = nullptr;
+    if (ri) {
+      if (ri->dim() != 1 || ri->size(0) == 0) return decline();
+      n_ref = ri->size(0);
+    }
+    if (L > 0) {
+      B = g.to_int(a[7]);
+      if (!g.ok || !q || q->dim() != 3) return decline();
+      const int64_t LB = (int64_t)L * B;
+      Hq = q->size(1);
+      qp = g.data3(q, bf16, dev, LB, Hq, kv.D);
+      klp = g.data3(kl, bf16, dev, LB, kv.Hkv, kv.D);
+      vlp = g.data3(vl, bf16, dev, LB, kv.Hkv, kv.D);
+      if (o) op = g.data3(o, bf16, dev, LB, Hq, kv.D);
+      lp = g.data2(lse, f32, dev, LB, Hq);
+    } else {
+      if (n_ref == 0 || !qr || qr->dim() != 3 || q || kl || vl || o || lse) return decline();
+      Hq = qr->size(1);
+    }
+    void *rip = nullptr, *qrp = nullptr, *krp = nullptr, *vrp = nullptr;
+    if (n_ref) {
+      rip = g.data(ri, at::kInt, dev);
+      qrp = g.data3(qr, bf16, dev, n_ref, Hq, kv.D);
+      krp = g.data3(kr, bf16, dev, n_ref, kv.Hkv, kv.D);
+      vrp = g.data3(vr, bf16, dev, n_ref, kv.Hkv, kv.D);
+      if (o_r) orp = g.data3(o_r, bf16, dev, n_ref, Hq, kv.D);
+      lrp = g.data2(lse_r, f32, dev, n_ref, Hq);
+    } else if (qr || kr || vr || o_r || lse_r) {
+      return decline();
+    }
+    if (Hq > INT32_MAX || n_ref > INT32_MAX) return decline();
+    if (!g.ok) return decline();
+    void* stream = g.stream_of(dev);
+    size_t bytes = 0;
+    const size_t need = f_attn_kv4_ws((int)L, B, P, (int)Hq, (int)kv.Hkv, (int)kv.D, (int)n_ref);
+    void* ws = g.ok ? workspace(g, a[18], "attn_kv4", need, *kc, dev, stream, &bytes, keep) : nullptr;
+    if (!g.ok) return decline();
+    if (L > 0 && !o) {
+      mo = at::empty({L * B, Hq, kv.D}, q->options());
+      op = mo.data_ptr();
+    }
+    if (L > 0 && !lse && want) {
+      ml = at::empty({L * B, Hq}, kc->options().dtype(f32));
+      lp = ml.data_ptr();
+    }
+    if (n_ref && !o_r) {
+      mor = at::empty({n_ref, Hq, kv.D}, qr->options());
+      orp = mor.data_ptr();
+    }
+    if (n_ref && !lse_r && want) {
+      mlr = at::empty({n_ref, Hq}, kc->options().dtype(f32));
+      lrp = mlr.data_ptr();
+    }
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = f_attn_kv4((al_bf16*)qp, (al_bf16*)klp, (al_bf16*)vlp, (uint8_t*)kv.codes, (uint8_t*)kv.scales, (int)kv.cap,
+                    L ? parent : nullptr, (int)L, B, P, (int)Hq, (int)kv.Hkv, (int)kv.D, scale, (int32_t*)rip,
+                    (int)n_ref, (al_bf16*)qrp, (al_bf16*)krp, (al_bf16*)vrp, (al_bf16*)orp, (float*)lrp, (al_bf16*)op,
+                    (float*)lp, ws, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (!status_ok(st, "lane_attn_forward_kv4")) return nullptr;
+    PyObject* t = PyTuple_New(4);
+    if (!t) return nullptr;
+    PyTuple_SET_ITEM(t, 0, wrap(o, a[13], mo));
+    PyTuple_SET_ITEM(t, 1, wrap(lse, a[14], ml));
+    PyTuple_SET_ITEM(t, 2, wrap(o_r, a[15], mor));
+    PyTuple_SET_ITEM(t, 3, wrap(lse_r, a[16], mlr));
+    return t;
+  });
+}
+
+// Shape of t with its last dimension n.
+std::vector<int64_t> with_last(const at::Tensor& t, int64_t n) {
+  auto v = t.sizes().vec();
+  v.back() = n;
+  return v;
+}
+bool same_shape(const at::Tensor* t, const at::Tensor& like, int64_t last) {
+  return !t || t->sizes() == at::IntArrayRef(with_last(like, last));
+}
+
+// quantize(x, codes, scales)
+PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  return guarded([&](PyObject**) -> PyObject* {
+    if (na != 3) return decline();
+    Args g;
+    const at::Tensor *x = g.tensor(a[0]), *c = g.tensor(a[1]), *s = g.tensor(a[2]);
+    if (!g.ok || !x || x->dim() < 1) return decline();
+    const int64_t n = x->size(-1);
+    if (n < 32 || n % 32 || n > INT32_MAX || !same_shape(c, *x, n / 2) || !same_shape(s, *x, n / 32)) return decline();
+    const int dev = current_device();
+    void *xp = g.data(x, at::kBFloat16, dev), *cp = g.data(c, at::kByte, dev), *sp = g.data(s, at::kByte, dev);
+    if (!g.ok) return decline();
+    void* stream = g.stream_of(dev);
+    if (!g.ok) return decline();
+    at::Tensor mc, ms;
+    if (!c) {
+      mc = at::empty(with_last(*x, n / 2), x->options().dtype(at::kByte));
+      cp = mc.data_ptr();
+    }
+    if (!s) {
+      ms = at::empty(with_last(*x, n / 32), x->options().dtype(at::kByte));
+      sp = ms.data_ptr();
+    }
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = f_quantize((al_bf16*)xp, x->numel() / n, (int)n, (uint8_t*)cp, (uint8_t*)sp, stream);
+    Py_END_ALLOW_THREADS
+    if (!status_ok(st, "mx4_quantize")) return nullptr;
+    PyObject* t = PyTuple_New(2);
+    if (!t) return nullptr;
+    PyTuple_SET_ITEM(t, 0, wrap(c, a[1], mc));
+    PyTuple_SET_ITEM(t, 1, wrap(s, a[2], ms));
+    return t;
+  });
+}
+
+// dequantize(codes, scales, y)
+PyObject* dequantize(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  return guarded([&](PyObject**) -> PyObject* {
+    if (na != 3) return decline();
+    Args g;
+    const at::Tensor *c = g.tensor(a[0]), *s = g.tensor(a[1]), *y = g.tensor(a[2]);
+    if (!g.ok || !c || !s || c->dim() < 1) return decline();
+    const int64_t n = 2 * c->size(-1);
+    if (n < 32 || n % 32 || n > INT32_MAX || !same_shape(s, *c, n / 32) || !same_shape(y, *c, n)) return decline();
+    const int dev = current_device();
+    void *cp = g.data(c, at::kByte, dev), *sp = g.data(s, at::kByte, dev), *yp = g.data(y, at::kBFloat16, dev);
+    if (!g.ok) return decline();
+    void* stream = g.stream_of(dev);
+    if (!g.ok) return decline();
+    at::Tensor my;
+    if (!y) {
+      my = at::empty(with_last(*c, n), c->options().dtype(at::kBFloat16));
+      yp = my.data_ptr();
+    }
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = f_dequantize((uint8_t*)cp, (uint8_t*)sp, 2 * c->numel() / n, (int)n, (al_bf16*)yp, stream);
+    Py_END_ALLOW_THREADS
+    if (!status_ok(st, "mx4_dequantize")) return nullptr;
+    return wrap(y, a[2], my);
+  });
+}
+
+// store(k, v, kv_codes, kv_scales, row_idx, start): True once enqueued.
+PyObject* store(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  return guarded([&](PyObject**) -> PyObject* {
+    if (na != 6) return decline();
+    Args g;
+    const at::Tensor *k = g.tensor(a[0]), *v = g.tensor(a[1]), *c = g.tensor(a[2]), *s = g.tensor(a[3]),
+                     *ri = g.tensor(a[4]);
+    const int start = g.to_int(a[5]);
+    if (!g.ok || !k || k->dim() != 3 || k->size(0) > INT32_MAX) return decline();
+    const int dev = current_device();
+    const Cache kv = cache_of(g, c, s, dev);
+    if (!g.ok) return decline();
+    const int64_t T = k->size(0);
+    void *kp = g.data3(k, at::kBFloat16, dev, T, kv.Hkv, kv.D), *vp = g.data3(v, at::kBFloat16, dev, T, kv.Hkv, kv.D);
+    if (ri && (ri->dim() != 1 || ri->size(0) != T)) return decline();
+    void* rp = g.data(ri, at::kInt, dev);
+    if (!g.ok) return decline();
+    void* stream = g.stream_of(dev);
+    if (!g.ok) return decline();
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = f_store((al_bf16*)kp, (al_bf16*)vp, (int32_t*)rp, start, (int)T, (int)kv.cap, (int)kv.Hkv, (int)kv.D,
+                 (uint8_t*)kv.codes, (uint8_t*)kv.scales, stream);
+    Py_END_ALLOW_THREADS
+    if (!status_ok(st, "kv4_store")) return nullptr;
+    Py_RETURN_TRUE;
   });
 }
 
@@ -463,6 +702,14 @@ PyObject* init(PyObject*, PyObject* args) {
   AL_GET(f_lm, "lmhead_confidence")
   AL_GET(f_lm_packed, "lmhead_confidence_packed")
   AL_GET(f_select, "select_unmask")
+  AL_GET(f_quantize, "mx4_quantize")
+  AL_GET(f_dequantize, "mx4_dequantize")
+  AL_GET(f_store, "kv4_store")
+  AL_GET(f_attn_kv4_ws, "lane_attn_kv4_workspace_size")
+  AL_GET(f_attn_kv4, "lane_attn_forward_kv4")
+  AL_GET(f_lm_mx4_size, "lmhead_packed_weight_mx4_size")
+  AL_GET(f_lm_mx4_ws, "lmhead_confidence_mx4_workspace_size")
+  AL_GET(f_lm_mx4, "lmhead_confidence_mx4")
 #undef AL_GET
   Py_XINCREF(check);
   Py_XINCREF(ws);
@@ -476,7 +723,12 @@ PyObject* init(PyObject*, PyObject* args) {
 PyMethodDef methods[] = {
     {"init", (PyCFunction)init, METH_VARARGS, nullptr},
     {"attn", (PyCFunction)(void (*)())attn, METH_FASTCALL, nullptr},
-    {"lmhead", (PyCFunction)(void (*)())lmhead, METH_FASTCALL, nullptr},
+    {"lmhead", (PyCFunction)(void (*)())lmhead<false>, METH_FASTCALL, nullptr},
+    {"lmhead_mx4", (PyCFunction)(void (*)())lmhead<true>, METH_FASTCALL, nullptr},
+    {"attn_kv4", (PyCFunction)(void (*)())attn_kv4, METH_FASTCALL, nullptr},
+    {"quantize", (PyCFunction)(void (*)())quantize, METH_FASTCALL, nullptr},
+    {"dequantize", (PyCFunction)(void (*)())dequantize, METH_FASTCALL, nullptr},
+    {"store", (PyCFunction)(void (*)())store, METH_FASTCALL, nullptr},
     {"select", (PyCFunction)(void (*)())select, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fast", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
