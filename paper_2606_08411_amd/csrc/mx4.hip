@@ -30,15 +30,16 @@ __global__ __launch_bounds__(MX_THREADS) void mx4_quantize_kernel(const i32x4* x
     i32x4 v[MX_SEGS];
 #pragma unroll
     for (int i = 0; i < MX_SEGS; ++i)   // n_seg is a multiple of 4: the lanes of a block stay together
-      if (base + i * MX_THREADS < n_seg) v[i] = x[base + i * MX_THREADS];
+      if (base + i * MX_THREADS < n_seg) v[i] = __builtin_nontemporal_load(x + base + i * MX_THREADS);
 #pragma unroll
     for (int i = 0; i < MX_SEGS; ++i)
       if (base + i * MX_THREADS < n_seg) put_segment(codes, scales, base + i * MX_THREADS, v[i]);
   }
 }
 
+template <bool NT>
 __global__ __launch_bounds__(MX_THREADS) void mx4_dequantize_kernel(const unsigned* codes, const uint8_t* scales,
-                                                                    long long n_seg, bf16x8* y) {
+                                                                    long long n_seg, i32x4* y) {
   const long long step = (long long)gridDim.x * MX_THREADS * MX_SEGS;
   for (long long base = (long long)blockIdx.x * MX_THREADS * MX_SEGS + threadIdx.x; base < n_seg; base += step) {
     unsigned c[MX_SEGS], s[MX_SEGS];
@@ -52,7 +53,11 @@ __global__ __launch_bounds__(MX_THREADS) void mx4_dequantize_kernel(const unsign
     }
 #pragma unroll
     for (int i = 0; i < MX_SEGS; ++i)
-      if (base + i * MX_THREADS < n_seg) y[base + i * MX_THREADS] = mx4_bf16x8(c[i], mx4_scale(s[i]));
+      if (base + i * MX_THREADS < n_seg) {
+        const i32x4 v = __builtin_bit_cast(i32x4, mx4_bf16x8(c[i], mx4_scale(s[i])));
+        if (NT) __builtin_nontemporal_store(v, y + base + i * MX_THREADS);
+        else y[base + i * MX_THREADS] = v;
+      }
   }
 }
 
@@ -89,8 +94,14 @@ hipError_t launch_mx4_quantize(const uint16_t* x, long long n, uint8_t* codes, u
 
 hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, long long n, uint16_t* y,
                                  hipStream_t stream) {
-  hipLaunchKernelGGL(mx4_dequantize_kernel, dim3(mx_blocks(n / 8, MX_THREADS * MX_SEGS)), dim3(MX_THREADS), 0, stream,
-                     reinterpret_cast<const unsigned*>(codes), scales, n / 8, reinterpret_cast<bf16x8*>(y));
+  // Values past 64 MB, more than the L2s hold, are stored non-temporally (and the
+  // quantiser's input, read once, is loaded so): 126464 x 4096 quantised and read back
+  // 472 us with neither, 471 and 467 with one, 406 with both; 46 MB of a cache 21.9 and
+  // 21.4 (MI355X).
+  const dim3 grid(mx_blocks(n / 8, MX_THREADS * MX_SEGS)), block(MX_THREADS);
+  const unsigned* c = reinterpret_cast<const unsigned*>(codes);
+  if (n > (32ll << 20)) hipLaunchKernelGGL(mx4_dequantize_kernel<true>, grid, block, 0, stream, c, scales, n / 8, reinterpret_cast<i32x4*>(y));
+  else hipLaunchKernelGGL(mx4_dequantize_kernel<false>, grid, block, 0, stream, c, scales, n / 8, reinterpret_cast<i32x4*>(y));
   return hipGetLastError();
 }
 
