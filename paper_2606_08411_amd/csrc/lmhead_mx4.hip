@@ -45,6 +45,22 @@ struct LmMx4Params {
 // so on) then touch every bank once.
 __device__ __forceinline__ int lm_slot(int c) { return (c & 3) | ((c & 8) ? 12 : 0); }
 
+// Over lanes l, l ^ 16, l ^ 32, l ^ 48; the same value on all four.
+__device__ __forceinline__ float quad_max(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return pair_max32(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return pair_sum32(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+__device__ __forceinline__ int quad_min(int v) {
+  const auto r = __builtin_amdgcn_permlane16_swap((unsigned)v, (unsigned)v, false, false);
+  const int w = min((int)r[0], (int)r[1]);
+  const auto t = __builtin_amdgcn_permlane32_swap((unsigned)w, (unsigned)w, false, false);
+  return min((int)t[0], (int)t[1]);
+}
+
 template <int CBT, int WC, int KS, int DEPTH, bool RAGGED, bool NT>
 __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
   constexpr int COLS = 16 * CBT;
@@ -229,27 +245,30 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
           const int n = nt * COLS + col;
           excl = (n < p.N && p.sup[n]) ? p.eos_id : -1;
         }
+        // The column's maximum over the four lanes that hold it, the first id that has
+        // it, and the sum of exponentials against it: no branches, no LDS.
         float m = -INFINITY;
-        int idx = 0x7fffffff;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int v = u * 64 + 16 * i + 4 * kb + r;
-            const float z = (v < ve && v != excl) ? acc[i][j][r] : -INFINITY;
-            acc[i][j][r] = z;
-            const bool gt = z > m;
-            m = gt ? z : m;
-            idx = gt ? v : idx;
+            acc[i][j][r] = (v < ve && v != excl) ? acc[i][j][r] : -INFINITY;
+            m = fmaxf(m, acc[i][j][r]);
           }
+        m = quad_max(m);
         const float m0 = (m == -INFINITY) ? 0.f : m;
         float s = 0.f;
+        int idx = 0x7fffffff;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 3; i >= 0; --i)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) s += exp2_fast((acc[i][j][r] - m0) * LM_LOG2E);
-        merge_state(m, s, idx, __shfl_xor(m, 16, kWave), __shfl_xor(s, 16, kWave), __shfl_xor(idx, 16, kWave));
-        merge_state(m, s, idx, __shfl_xor(m, 32, kWave), __shfl_xor(s, 32, kWave), __shfl_xor(idx, 32, kWave));
+          for (int r = 3; r >= 0; --r) {
+            idx = acc[i][j][r] == m ? u * 64 + 16 * i + 4 * kb + r : idx;
+            s += exp2_fast((acc[i][j][r] - m0) * LM_LOG2E);
+          }
+        s = quad_sum(s);
+        idx = quad_min(idx);
         if (kb == 0) {
           red_m[wr * COLS + col] = m;
           red_s[wr * COLS + col] = s;
@@ -259,10 +278,20 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
     }
     __syncthreads();
     for (int col = tid; col < COLS; col += TH) {
-      float m = red_m[col], s = red_s[col];
-      int idx = red_i[col];
-      for (int i = 1; i < u_end - u_begin; ++i)
-        merge_state(m, s, idx, red_m[i * COLS + col], red_s[i * COLS + col], red_i[i * COLS + col]);
+      const int n = u_end - u_begin;
+      float mu[WR], m = -INFINITY, s = 0.f;
+      int idx = 0x7fffffff;
+#pragma unroll
+      for (int i = 0; i < WR; ++i) {
+        mu[i] = i < n ? red_m[i * COLS + col] : -INFINITY;
+        m = fmaxf(m, mu[i]);
+      }
+#pragma unroll
+      for (int i = WR - 1; i >= 0; --i) {
+        const bool some = mu[i] != -INFINITY;   // (a unit whose only row is a suppressed EOS has none)
+        s += some ? red_s[i * COLS + col] * exp2_fast((mu[i] - m) * LM_LOG2E) : 0.f;
+        idx = some && mu[i] == m ? red_i[i * COLS + col] : idx;
+      }
       LmPartial q;
       q.m = m;
       q.s = s;
