@@ -169,7 +169,7 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
     // but the loads issued after them: W twice and one group of hidden rows),
     // everyone is done with the group before, and its buffer takes the hidden rows
     // of the group after next.
-    const int n_group = (p.n_st + KS - 1) / KS, n_run = (n_group + DEPTH - 1) / DEPTH * DEPTH;
+    const int n_group = (p.n_st + KS - 1) / KS;
     int slot = 0;   // byte of the ring
     auto next_slot = [&](int x, int by) {
       x += by * KS * HB;
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
     if (!active) {
       load_hidden(0, 0);
       load_hidden(1, KS * HB);
-      for (int i = 0; i < n_run; ++i) {
+      for (int i = 0; i < n_group; ++i) {
         wait_loads_and_barrier<LH>();
         load_hidden(i + 2, next_slot(slot, 2));
         slot = next_slot(slot, 1);
@@ -193,18 +193,22 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
       load_hidden(0, 0);
       load_hidden(1, KS * HB);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      for (int i0 = 0; i0 < n_run; i0 += DEPTH) {
-#pragma unroll
-        for (int q = 0; q < DEPTH; ++q) {
-          const int i = i0 + q;
+      // (One group inside the other's condition: no path leaves one out and takes a
+      // later one, so the compiler's waits for W stay exact too.)
+      auto step = [&](auto self, auto q_tag, int i0) -> void {
+        constexpr int q = decltype(q_tag)::value;
+        const int i = i0 + q;
+        if (i < n_group) {
           wait_loads_and_barrier<10 + LH>();
           load_hidden(i + 2, next_slot(slot, 2));
           load_w(g[(q + DEPTH - 1) % DEPTH], (i + DEPTH - 1) * KS + ks);
           __builtin_amdgcn_sched_barrier(0);
-          if (i * KS + ks < p.n_st) compute(g[q], slot + ks * HB);
+          if (KS == 1 || i * KS + ks < p.n_st) compute(g[q], slot + ks * HB);
           slot = next_slot(slot, 1);
+          if constexpr (q + 1 < DEPTH) self(self, IntTag<q + 1>{}, i0);
         }
-      }
+      };
+      for (int i0 = 0; i0 < n_group; i0 += DEPTH) step(step, IntTag<0>{}, i0);
     }
     wait_loads_and_barrier<0>();   // (the last loads land in the ring too)
     // The KS partial sums of a tile, in ascending order of ks.
