@@ -1083,7 +1083,7 @@ static hipError_t run_pass(const AttnParams& base, const PassShape& s, const Att
 // 32 over 2048 37.0 -> 36.7, 12 of 64 over 1500 21.8 -> 22.3; chains the same.
 // Lane i's parent is the highest of its ancestors (parents come first); any
 // order is correct.
-static void dfs_order(const unsigned long long* vis, int L, unsigned* order) {
+void attn_dfs_order(const unsigned long long* vis, int L, unsigned* order) {
   unsigned long long children[AT_MAX_LANES + 1] = {};   // (the last: roots)
   for (int i = 0; i < L; ++i) {
     const unsigned long long anc = vis[i] & ((1ull << i) - 1);
@@ -1154,7 +1154,7 @@ hipError_t launch_lane_attention(const uint16_t* q, const uint16_t* k_lane, cons
   p.n_key_lanes = L;
   p.lane_key_tiles = (B + AT_KT - 1) / AT_KT;
   for (int i = 0; i < L; ++i) p.vis[i] = vis[i];
-  if (L > 0 && !pl.wsplit_lane) dfs_order(vis, L, p.order);
+  if (L > 0 && !pl.wsplit_lane) attn_dfs_order(vis, L, p.order);
   hipError_t e = hipSuccess;
   if (L > 0) {  // L = 0: refresh-only call
     const PassShape a = pass_shape(L * B, B, L, g, Hkv, P, B, L);

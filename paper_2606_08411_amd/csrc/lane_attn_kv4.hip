@@ -54,7 +54,11 @@ struct Kv4Params {
   int tpw;                  // tile kernel: query tiles (computing wavefronts) per workgroup
   float scale_log2;
   unsigned long long vis[64];    // bit j: lane block j visible to lane i
+  // The lanes in the order in which their rows are listed as pairs (depth first, so
+  // that neighbours share most of their ancestors), four to a word.
+  unsigned order[16];
 };
+__device__ __forceinline__ int lane_at(const Kv4Params& p, int pos) { return (p.order[pos >> 2] >> (8 * (pos & 3))) & 255; }
 
 // Bits of the KT lane rows from `row` on that a pair with visibility v sees.
 template <int KT>
@@ -78,9 +82,15 @@ struct Pair {
 __device__ __forceinline__ Pair pair_at(const Kv4Params& p, int hk, int x) {
   Pair q;
   q.ok = x < p.n_pairs;
-  q.row = q.ok ? x / p.g : 0;
-  q.hq = hk * p.g + (q.ok ? x - q.row * p.g : 0);
-  q.vis = q.ok && p.R > 0 ? p.vis[q.row / p.B] : 0;
+  const int r = q.ok ? x / p.g : 0;
+  q.hq = hk * p.g + (q.ok ? x - r * p.g : 0);
+  q.row = r;
+  q.vis = 0;
+  if (p.R > 0) {
+    const int pos = r / p.B, l = lane_at(p, pos);
+    q.row = l * p.B + r - pos * p.B;
+    if (q.ok) q.vis = p.vis[l];
+  }
   return q;
 }
 // Lane blocks that some pair of [x0, x1) sees.
@@ -88,7 +98,7 @@ __device__ __forceinline__ unsigned long long blocks_seen(const Kv4Params& p, in
   unsigned long long v = 0;
   if (p.R > 0 && x0 < p.n_pairs) {
     const int l1 = (min(x1, p.n_pairs) - 1) / p.g / p.B;
-    for (int l = x0 / p.g / p.B; l <= l1; ++l) v |= p.vis[l];
+    for (int l = x0 / p.g / p.B; l <= l1; ++l) v |= p.vis[lane_at(p, l)];
   }
   return v;
 }
@@ -642,8 +652,8 @@ void lane_attn_kv4_unit_kernel(Kv4Params p) {
         acc[4 + e] += b[e] * wgt;
       }
     }
-    const int row = (x0 + r) / p.g;
-    const size_t orow = (size_t)row * p.Hq + hk * p.g + (x0 + r - row * p.g);
+    const Pair out_pair = pair_at(p, hk, x0 + r);
+    const size_t orow = (size_t)out_pair.row * p.Hq + out_pair.hq;
     if (p.n_split == 1) {
       const float inv = 1.0f / L;
       bf16x8 out;
@@ -724,9 +734,22 @@ static Kv4Pass kv4_pass(int n_rows, int R, int P, int Hq, int Hkv, int D) {
   } else {
     s.n_pre = (P + K4_KT - 1) / K4_KT;
     s.n_tiles = s.n_pre + (R + K4_KT - 1) / K4_KT;
-    s.tpw = K4_WAVES;
-    const long long wgs = (q_tiles + s.tpw - 1) / s.tpw * Hkv;
-    while (s.n_split < 16 && wgs * s.n_split < 256 && s.n_tiles >= 6 * s.n_split) s.n_split *= 2;
+    // The cheapest of 8 or 4 query tiles a workgroup and 1 to 16 splits, in us
+    // (MI355X): a key tile costs 1.9 with 8, 1.1 with 4 (two thirds of it at D = 64), a
+    // round of one workgroup per compute unit 5, a split its partials and a merge.
+    double best = 1e30;
+    for (int t = K4_WAVES; t >= 4; t /= 2)
+      for (int ns = 1; ns <= 16 && (ns == 1 || s.n_tiles >= 3 * ns); ns *= 2) {
+        const long long wgs = (q_tiles + t - 1) / t * Hkv * ns;
+        const double tile = (t == K4_WAVES ? 1.9 : 1.1) * (D == 64 ? 0.68 : 1.0);
+        const double cost = (double)((wgs + 255) / 256) * ((s.n_tiles + ns - 1) / ns * tile + 5.0) +
+                            (ns > 1 ? 5.0 + 1.7e-6 * ns * n_rows * (double)Hq * D : 0.0);
+        if (cost < best) {
+          best = cost;
+          s.tpw = t;
+          s.n_split = ns;
+        }
+      }
   }
   s.ws = s.n_split > 1 ? (size_t)s.n_split * n_rows * Hq * (D + 2) * sizeof(float) : 0;
   return s;
@@ -798,6 +821,7 @@ hipError_t launch_lane_attn_kv4(const uint16_t* q, const uint16_t* k_lane, const
     p.R = L * B;
     p.B = B;
     for (int i = 0; i < L; ++i) p.vis[i] = vis[i];
+    attn_dfs_order(vis, L, p.order);
     const Kv4Pass s = kv4_pass(L * B, L * B, P, Hq, Hkv, D);
     const hipError_t e = D == 64 ? run_kv4_pass<64>(p, s, ws, stream) : run_kv4_pass<128>(p, s, ws, stream);
     if (e != hipSuccess) return e;

@@ -31,6 +31,9 @@ hipError_t launch_lane_attention(const uint16_t* q, const uint16_t* k_lane, cons
                                  float* lse_ref, uint16_t* o, float* lse, void* ws,
                                  hipStream_t stream);
 
+// Lanes depth first, four to a word of order (zeroed, 16 words).
+void attn_dfs_order(const unsigned long long* vis, int L, unsigned* order);
+
 // ---- LM head
 size_t lmhead_workspace_bytes(int N, int d, int V);
 // Device address (current device) of the fixed partials array used by
