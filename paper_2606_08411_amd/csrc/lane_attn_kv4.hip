@@ -131,7 +131,10 @@ void lane_attn_kv4_kernel(Kv4Params p) {
   constexpr int SEGS = D / 8;       // 16-byte segments of a row
   constexpr int NL = 2 * K4_KT * SEGS / K4_THREADS;   // bf16 segments per thread of a lane tile
   constexpr int AHEAD = 4;          // K fragments read ahead
-  __shared__ __attribute__((aligned(1024))) char lds[6 * TB];   // three buffers of K then V
+  // Fragments of q kept in LDS: at D = 128 the registers hold all but the last two (with all
+  // of them the compiler spills two, and their reloads wait for every load in flight).
+  constexpr int QL = D == 128 ? 2 : 0, QR = KS - QL;
+  __shared__ __attribute__((aligned(1024))) char lds[6 * TB + QL * K4_WAVES * 1024];   // three buffers of K then V, q
 
   const int hk = blockIdx.y, split = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -142,12 +145,18 @@ void lane_attn_kv4_kernel(Kv4Params p) {
   const Pair pr = pair_at(p, hk, w < p.tpw ? x0 + w * 32 + r32 : p.n_pairs);
   const unsigned long long wg_vis = blocks_seen(p, x0, x0 + 32 * p.tpw);
 
-  bf16x8 qf[KS];
+  bf16x8 qr[QR];
+  bf16x8* const ql = reinterpret_cast<bf16x8*>(lds + 6 * TB) + w * kWave + lane;   // (this lane's own)
   {
     const uint16_t* qrow = p.q + ((size_t)pr.row * p.Hq + pr.hq) * D;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = pr.ok ? load_bf16x8(qrow + ks * 16 + hh * 8) : zero_bf16x8();
+    for (int ks = 0; ks < KS; ++ks) {
+      const bf16x8 v = pr.ok ? load_bf16x8(qrow + ks * 16 + hh * 8) : zero_bf16x8();
+      if (ks < QR) qr[ks] = v;
+      else ql[(ks - QR) * K4_THREADS] = v;
+    }
   }
+  auto qf = [&](int ks) -> bf16x8 { return ks < QR ? qr[ks < QR ? ks : 0] : ql[(ks - QR) * K4_THREADS]; };
   f32x16 oacc[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -166,18 +175,18 @@ void lane_attn_kv4_kernel(Kv4Params p) {
     i32x4 x;
     unsigned s;
   };
-  constexpr int NP = 2 * K4_KT * DT;   // 16-byte pieces of codes of a tile (at D = 64 half the threads have none)
-  const int prow = (tid & (NP / 2 - 1)) / DT, pblk = tid & (DT - 1), pv = tid / (NP / 2);
-  const bool stager = NP == K4_THREADS || tid < NP;
-  const size_t pat = (((size_t)(stager ? pv : 0) * p.Hkv + hk) * p.cap + prow) * DT + pblk;
-  auto load_codes = [&](Codes& g, int t) {   // (rows past the prefix are zero)
-    g.x = i32x4{0, 0, 0, 0};
-    g.s = 0;
-    if (stager && t * K4_KT + prow < p.P) {
-      const size_t at = pat + (size_t)t * (K4_KT * DT);
-      g.x = reinterpret_cast<const i32x4*>(p.codes)[at];
-      g.s = p.scales[at];
-    }
+  // (At D = 64 there are 256 pieces: threads 256 .. 511 do those of 0 .. 255 again.  A
+  // row past the prefix repeats the last one; its P is 0.  No branches: where two
+  // paths meet the compiler waits for LDS as if the longer one had been taken.)
+  constexpr int NP = 2 * K4_KT * DT;   // 16-byte pieces of codes of a tile
+  const int pidx = tid & (NP / 2 - 1), prow = pidx / DT, pblk = pidx & (DT - 1);
+  const int pv = (w / (NP / 2 / kWave)) & 1;   // K or V, the same for a whole wavefront
+  const size_t phead = ((size_t)pv * p.Hkv + hk) * p.cap;
+  auto load_codes = [&](Codes& g, int t) {
+    const size_t at = (phead + (size_t)t * K4_KT) * DT;   // (uniform)
+    const unsigned off = min(prow, p.P - 1 - t * K4_KT) * DT + pblk;
+    g.x = reinterpret_cast<const i32x4*>(p.codes)[at + off];
+    g.s = p.scales[at + off];
   };
   const int pdst = pv * TB + prow * ROWB, pf = pv ? fv(prow) : fk(prow);
   auto store_piece = [&](const Codes& g, int buf, int j) {   // j = 0..3
@@ -185,10 +194,8 @@ void lane_attn_kv4_kernel(Kv4Params p) {
         mx4_bf16x8((unsigned)g.x[j], mx4_scale(g.s));
   };
   auto store_codes = [&](const Codes& g, int buf) {
-    if (stager) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) store_piece(g, buf, j);
-    }
+    for (int j = 0; j < 4; ++j) store_piece(g, buf, j);
   };
   auto load_rows = [&](i32x4 (&x)[NL], int t) {   // of lane tile t: K rows, then V rows
     const int r0 = (t - p.n_pre) * K4_KT;
@@ -221,20 +228,33 @@ void lane_attn_kv4_kernel(Kv4Params p) {
   auto kread = [&](int buf, int i) {
     return *reinterpret_cast<const bf16x8*>(lds + buf * 2 * TB + (ka ^ (32 * (i >> 1))) + (i & 1) * 32 * ROWB);
   };
-  auto vfrag = [&](int buf, int ks2, int dt) {
-    const uint16_t* a = reinterpret_cast<const uint16_t*>(lds + buf * 2 * TB + TB + (va ^ (64 * dt)) + 16 * ks2 * ROWB);
+  auto vfrag = [&](int buf, int ks2, int dt, int half = 0) {
+    const uint16_t* a = reinterpret_cast<const uint16_t*>(lds + buf * 2 * TB + TB + (va ^ (64 * dt)) +
+                                                          (16 * ks2 + 32 * half) * ROWB);
     return cat_bf16x4(lds_read_tr16(a), lds_read_tr16(a + 8 * D));
   };
   const f32x16 zero16 = {};
   auto qk = [&](Scores& sc, int buf) {
 #pragma unroll
     for (int i = 0; i < 2 * KS; ++i)
-      sc.s[i & 1] = mfma32x32x16(kread(buf, i), qf[i >> 1], i < 2 ? zero16 : sc.s[i & 1]);
+      sc.s[i & 1] = mfma32x32x16(kread(buf, i), qf(i >> 1), i < 2 ? zero16 : sc.s[i & 1]);
   };
-  auto mask = [&](Scores& sc, unsigned long long km) {
+  auto qk_half = [&](Scores& sc, int buf, int half) {   // keys 32 half .. 32 half + 31, into s[0]
+    const char* kt = lds + buf * 2 * TB + half * 32 * ROWB;
+    f32x16 s1 = zero16;   // (two chains)
+    sc.s[0] = zero16;
+#pragma unroll
+    for (int i = 0; i < KS; i += 2) {
+      sc.s[0] = mfma32x32x16(*reinterpret_cast<const bf16x8*>(kt + (ka ^ (32 * i))), qf(i), sc.s[0]);
+      s1 = mfma32x32x16(*reinterpret_cast<const bf16x8*>(kt + (ka ^ (32 * (i + 1)))), qf(i + 1), s1);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc.s[0][r] += s1[r];
+  };
+  auto mask = [&](auto nh_tag, Scores& sc, unsigned long long km) {   // (of NH = 1 or 2 halves)
     const unsigned mw[2] = {(unsigned)km >> (4 * hh), (unsigned)(km >> 32) >> (4 * hh)};
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < decltype(nh_tag)::value; ++kb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) sc.s[kb][r] = mw[kb] & (1u << (8 * (r >> 2) + (r & 3))) ? sc.s[kb][r] : -INFINITY;
   };
@@ -272,19 +292,21 @@ void lane_attn_kv4_kernel(Kv4Params p) {
   // O^T += V^T P^T, the second half of P's exponentials between the MFMAs of the
   // first two steps and, where a prefix tile is to be stored, its pieces between
   // those of the last two.  vf[0] holds the first step's fragments.
-  auto pv_product = [&](auto store_tag, const Scores& sc, bf16x8* pk, bf16x8 (*vf)[DT], float m_use, float alpha,
-                        float rs, int buf, const Codes& g, int sbuf) {   // (sbuf < 0: nothing to store)
+  // (NH = 1: the 32 keys of one half alone, their exponentials done.)
+  auto pv_product = [&](auto nh_tag, auto store_tag, const Scores& sc, bf16x8* pk, bf16x8 (*vf)[DT], float m_use,
+                        float alpha, float rs, int buf, int half, const Codes& g, int sbuf) {
+    constexpr int NH = decltype(nh_tag)::value;
 #pragma unroll
-    for (int ks2 = 0; ks2 < 4; ++ks2) {
+    for (int ks2 = 0; ks2 < 2 * NH; ++ks2) {
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        if (ks2 < 3) vf[(ks2 + 1) & 1][dt] = vfrag(buf, ks2 + 1, dt);
+        if (ks2 < 2 * NH - 1) vf[(ks2 + 1) & 1][dt] = vfrag(buf, ks2 + 1, dt, half);
         oacc[dt] = mfma32x32x16(vf[ks2 & 1][dt], pk[ks2], oacc[dt]);
-        if (ks2 < 2) {
+        if (NH == 2 && ks2 < 2) {
 #pragma unroll
           for (int q = 0; q < 4 / DT; ++q) exp_pair(sc, pk, m_use, rs, 8 + ks2 * 4 + dt * (4 / DT) + q);
         } else if (decltype(store_tag)::value && (dt & (DT / 2 - 1)) == 0) {
-          if (stager && sbuf >= 0) store_piece(g, sbuf, 2 * (ks2 - 2) + dt / (DT / 2));
+          store_piece(g, sbuf, 2 * (ks2 - 2) + dt / (DT / 2));
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -305,7 +327,7 @@ void lane_attn_kv4_kernel(Kv4Params p) {
     for (int i = 0; i < 2 * KS; ++i) {
       if (i + AHEAD < 2 * KS) kf[i + AHEAD] = kread(bq, i + AHEAD);
       else if (i + DT >= 2 * KS) vf[0][i + DT - 2 * KS] = vfrag(bv, 0, i + DT - 2 * KS);
-      nxt.s[i & 1] = mfma32x32x16(kf[i], qf[i >> 1], i < 2 ? zero16 : nxt.s[i & 1]);
+      nxt.s[i & 1] = mfma32x32x16(kf[i], qf(i >> 1), i < 2 ? zero16 : nxt.s[i & 1]);
       if (i < MX) {
 #pragma unroll
         for (int q = 0; q < 4 / MX; ++q) mx = max_piece(mx, cur, i * (4 / MX) + q);
@@ -323,21 +345,22 @@ void lane_attn_kv4_kernel(Kv4Params p) {
       __builtin_amdgcn_sched_barrier(0);
     }
     rescale(alpha);
-    pv_product(IntTag<1>{}, cur, pk, vf, m_use, alpha, rs, bv, g, sbuf);
+    pv_product(IntTag<2>{}, IntTag<1>{}, cur, pk, vf, m_use, alpha, rs, bv, 0, g, sbuf);
   };
-  auto cold_tile = [&](const Scores& cur, int bv) {   // softmax and P V alone
+  auto cold_tile = [&](auto nh_tag, const Scores& cur, int bv, int half) {   // softmax and P V alone
+    constexpr int NH = decltype(nh_tag)::value;
     bf16x8 pk[4], vf[2][DT];
     float mx = -INFINITY, m_use, rs = 0.f;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) mx = max_piece(mx, cur, q);
+    for (int q = 0; q < 2 * NH; ++q) mx = max_piece(mx, cur, q);
     const float alpha = new_max(mx, m_use);
 #pragma unroll
     for (int q = 0; q < 8; ++q) exp_pair(cur, pk, m_use, rs, q);
     rescale(alpha);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) vf[0][dt] = vfrag(bv, 0, dt);
+    for (int dt = 0; dt < DT; ++dt) vf[0][dt] = vfrag(bv, 0, dt, half);
     __builtin_amdgcn_sched_barrier(0);
-    pv_product(IntTag<0>{}, cur, pk, vf, m_use, alpha, rs, bv, Codes{}, -1);
+    pv_product(nh_tag, IntTag<0>{}, cur, pk, vf, m_use, alpha, rs, bv, half, Codes{}, 0);
   };
 
   // This split's tiles: prefix tiles [t0, pe), then the lane tiles that some pair of
@@ -352,20 +375,19 @@ void lane_attn_kv4_kernel(Kv4Params p) {
     Codes g;
     load_codes(g, t0);
     store_codes(g, 0);
-    if (t0 + 1 < pe) {
-      load_codes(g, t0 + 1);
-      store_codes(g, 1);
-    }
-    if (t0 + 2 < pe) load_codes(g, t0 + 2);
+    load_codes(g, min(t0 + 1, pe - 1));
+    store_codes(g, 1);
+    load_codes(g, min(t0 + 2, pe - 1));
     __syncthreads();
     Scores sa, sb;
     if (computing) qk(sa, 0);
     int t = t0, buf = 0;
     auto step = [&](Scores& cur, Scores& nxt) {   // t + 1 < pe
-      const int sbuf = t + 2 < pe ? third(buf + 2) : -1;
+      // (Past the last tile its codes are stored once more, in a buffer that nobody reads.)
+      const int sbuf = third(buf + 2);
       if (computing) hot_tile(cur, nxt, third(buf + 1), buf, g, sbuf);
-      else if (sbuf >= 0) store_codes(g, sbuf);
-      if (t + 3 < pe) load_codes(g, t + 3);
+      else store_codes(g, sbuf);
+      load_codes(g, min(t + 3, pe - 1));
       // (__syncthreads would wait for the loads too)
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       ++t;
@@ -373,8 +395,8 @@ void lane_attn_kv4_kernel(Kv4Params p) {
     };
     auto last = [&](Scores& cur) {
       if (computing) {
-        if (p.P - t * K4_KT < K4_KT) mask(cur, (1ull << (p.P - t * K4_KT)) - 1);
-        cold_tile(cur, buf);
+        if (p.P - t * K4_KT < K4_KT) mask(IntTag<2>{}, cur, (1ull << (p.P - t * K4_KT)) - 1);
+        cold_tile(IntTag<2>{}, cur, buf, 0);
       }
     };
     while (t + 2 < pe) {   // (two at a time: the scores keep their registers)
@@ -401,11 +423,17 @@ void lane_attn_kv4_kernel(Kv4Params p) {
     if (tn < t_end) load_rows(rows, tn);
     if (computing) {
       const unsigned long long km = key_mask<K4_KT>(pr.vis, (t - p.n_pre) * K4_KT, p.B, p.R);
-      if (__ballot(km != 0)) {
-        Scores sc;
+      // A half that no pair of the wavefront sees is left out.
+      const bool lo = __ballot((unsigned)km != 0) != 0, hi = __ballot((unsigned)(km >> 32) != 0) != 0;
+      Scores sc;
+      if (lo && hi) {
         qk(sc, buf);
-        mask(sc, km);
-        cold_tile(sc, buf);
+        mask(IntTag<2>{}, sc, km);
+        cold_tile(IntTag<2>{}, sc, buf, 0);
+      } else if (lo || hi) {
+        qk_half(sc, buf, hi);
+        mask(IntTag<1>{}, sc, hi ? km >> 32 : km);
+        cold_tile(IntTag<1>{}, sc, buf, hi);
       }
     }
     if (tn < t_end) store_rows(rows, buf ^ 1);
