@@ -51,7 +51,6 @@ struct Kv4Params {
   int n_rows, R, B, P, cap, Hq, Hkv, g;
   int n_pairs;              // n_rows * g
   int n_pre, n_tiles, n_split;   // prefix tiles (units), all key tiles (units)
-  int tpw;                  // tile kernel: query tiles (computing wavefronts) per workgroup
   float scale_log2;
   unsigned long long vis[64];    // bit j: lane block j visible to lane i
   // The lanes in the order in which their rows are listed as pairs (depth first, so
@@ -121,7 +120,11 @@ __device__ __forceinline__ int next_visible(const Kv4Params& p, unsigned long lo
 // multiplies K of tile i + 1 while the softmax of tile i runs between the MFMAs, then
 // V of tile i, with the conversion of tile i + 2 between the last of them.  Three
 // buffers, one barrier a tile.
-template <int D>
+//
+// Eight query tiles (TPW): every wavefront computes and stages an eighth of each
+// tile.  Four: wavefronts 0 .. 3 compute, 4 .. 7 stage.  (Window of 2563 refreshed
+// rows x 32 heads, three rounds of 4: ... us with the computing wavefronts staging.)
+template <int D, int TPW>
 __global__ __launch_bounds__(K4_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void lane_attn_kv4_kernel(Kv4Params p) {
   constexpr int KS = D / 16;        // MFMA k-steps of S^T = K Q^T
@@ -129,7 +132,8 @@ void lane_attn_kv4_kernel(Kv4Params p) {
   constexpr int ROWB = 2 * D;       // bytes of a K or V row in LDS
   constexpr int TB = K4_KT * ROWB;
   constexpr int SEGS = D / 8;       // 16-byte segments of a row
-  constexpr int NL = 2 * K4_KT * SEGS / K4_THREADS;   // bf16 segments per thread of a lane tile
+  constexpr int ST = TPW == K4_WAVES ? K4_THREADS : K4_THREADS / 2;   // staging threads
+  constexpr int NL = 2 * K4_KT * SEGS / ST;           // bf16 segments per staging thread of a lane tile
   constexpr int AHEAD = 4;          // K fragments read ahead
   // Fragments of q kept in LDS: at D = 128 the registers hold all but the last two (with all
   // of them the compiler spills two, and their reloads wait for every load in flight).
@@ -140,10 +144,11 @@ void lane_attn_kv4_kernel(Kv4Params p) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r32 = lane & 31, hh = lane >> 5, lgrp = lane >> 4, lg = lane & 15;
-  const int x0 = blockIdx.x * 32 * p.tpw;
-  const bool computing = w < p.tpw && x0 + w * 32 < p.n_pairs;
-  const Pair pr = pair_at(p, hk, w < p.tpw ? x0 + w * 32 + r32 : p.n_pairs);
-  const unsigned long long wg_vis = blocks_seen(p, x0, x0 + 32 * p.tpw);
+  const int x0 = blockIdx.x * 32 * TPW;
+  const bool computing = w < TPW && x0 + w * 32 < p.n_pairs;
+  const bool staging = TPW == K4_WAVES || w >= TPW;
+  const Pair pr = pair_at(p, hk, w < TPW ? x0 + w * 32 + r32 : p.n_pairs);
+  const unsigned long long wg_vis = blocks_seen(p, x0, x0 + 32 * TPW);
 
   bf16x8 qr[QR];
   bf16x8* const ql = reinterpret_cast<bf16x8*>(lds + 6 * TB) + w * kWave + lane;   // (this lane's own)
@@ -171,49 +176,55 @@ void lane_attn_kv4_kernel(Kv4Params p) {
   auto fv = [](int r) {
     return D == 128 ? (4 * (r & 3)) ^ (2 * ((r >> 2) & 1)) : (4 * ((r >> 1) & 1)) ^ (2 * ((r >> 2) & 1));
   };
-  struct Codes {      // of a prefix tile: this thread's 32 elements
+  struct Codes {      // of a prefix tile: 32 elements
     i32x4 x;
     unsigned s;
   };
-  // (At D = 64 there are 256 pieces: threads 256 .. 511 do those of 0 .. 255 again.  A
-  // row past the prefix repeats the last one; its P is 0.  No branches: where two
-  // paths meet the compiler waits for LDS as if the longer one had been taken.)
+  // (At D = 64 and eight query tiles there are 256 pieces: threads 256 .. 511 do those
+  // of 0 .. 255 again.  A row past the prefix repeats the last one; its P is 0.  No
+  // branches: where two paths meet the compiler waits for LDS as if the longer one
+  // had been taken.)
   constexpr int NP = 2 * K4_KT * DT;   // 16-byte pieces of codes of a tile
+  constexpr int NC = NP > ST ? NP / ST : 1;   // per staging thread: 1, or 2 (K and V)
   const int pidx = tid & (NP / 2 - 1), prow = pidx / DT, pblk = pidx & (DT - 1);
-  const int pv = (w / (NP / 2 / kWave)) & 1;   // K or V, the same for a whole wavefront
-  const size_t phead = ((size_t)pv * p.Hkv + hk) * p.cap;
-  auto load_codes = [&](Codes& g, int t) {
-    const size_t at = (phead + (size_t)t * K4_KT) * DT;   // (uniform)
+  const int pv = NC == 2 ? 0 : (w / (NP / 2 / kWave)) & 1;   // K or V, the same for a whole wavefront
+  auto load_codes = [&](Codes (&g)[NC], int t) {
     const unsigned off = min(prow, p.P - 1 - t * K4_KT) * DT + pblk;
-    g.x = reinterpret_cast<const i32x4*>(p.codes)[at + off];
-    g.s = p.scales[at + off];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const size_t at = (((size_t)(pv + c) * p.Hkv + hk) * p.cap + (size_t)t * K4_KT) * DT;   // (uniform)
+      g[c].x = reinterpret_cast<const i32x4*>(p.codes)[at + off];
+      g[c].s = p.scales[at + off];
+    }
   };
   const int pdst = pv * TB + prow * ROWB, pf = pv ? fv(prow) : fk(prow);
-  auto store_piece = [&](const Codes& g, int buf, int j) {   // j = 0..3
-    *reinterpret_cast<bf16x8*>(lds + buf * 2 * TB + pdst + ((4 * pblk + j) ^ pf) * 16) =
+  auto store_piece = [&](const Codes& g, int dst, int f, int buf, int j) {   // j = 0..3
+    *reinterpret_cast<bf16x8*>(lds + buf * 2 * TB + dst + ((4 * pblk + j) ^ f) * 16) =
         mx4_bf16x8((unsigned)g.x[j], mx4_scale(g.s));
   };
-  auto store_codes = [&](const Codes& g, int buf) {
+  auto store_codes = [&](const Codes (&g)[NC], int buf) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) store_piece(g, buf, j);
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) store_piece(g[c], pdst + c * TB, c ? fv(prow) : pf, buf, j);
   };
+  const int sid = tid & (ST - 1);
   auto load_rows = [&](i32x4 (&x)[NL], int t) {   // of lane tile t: K rows, then V rows
     const int r0 = (t - p.n_pre) * K4_KT;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int seg = tid + i * K4_THREADS;
+      const int seg = sid + i * ST;
       const int sr = (seg / SEGS) % K4_KT, sv = seg / (SEGS * K4_KT);
       const uint16_t* base = sv ? p.v_lane : p.k_lane;
-      x[i] = i32x4{0, 0, 0, 0};
-      if (r0 + sr < p.R)
-        x[i] = *reinterpret_cast<const i32x4*>(base + ((size_t)(r0 + sr) * p.Hkv + hk) * D + (seg % SEGS) * 8);
+      // (A row past the last repeats it; nobody sees it.)
+      x[i] = *reinterpret_cast<const i32x4*>(base + ((size_t)min(r0 + sr, p.R - 1) * p.Hkv + hk) * D + (seg % SEGS) * 8);
     }
   };
   auto store_rows = [&](const i32x4 (&x)[NL], int buf) {
     char* b = lds + buf * 2 * TB;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int seg = tid + i * K4_THREADS;
+      const int seg = sid + i * ST;
       const int sr = (seg / SEGS) % K4_KT, sv = seg / (SEGS * K4_KT);
       *reinterpret_cast<i32x4*>(b + sv * TB + sr * ROWB + ((seg % SEGS) ^ (sv ? fv(sr) : fk(sr))) * 16) = x[i];
     }
@@ -294,7 +305,7 @@ void lane_attn_kv4_kernel(Kv4Params p) {
   // those of the last two.  vf[0] holds the first step's fragments.
   // (NH = 1: the 32 keys of one half alone, their exponentials done.)
   auto pv_product = [&](auto nh_tag, auto store_tag, const Scores& sc, bf16x8* pk, bf16x8 (*vf)[DT], float m_use,
-                        float alpha, float rs, int buf, int half, const Codes& g, int sbuf) {
+                        float alpha, float rs, int buf, int half, const Codes (&g)[NC], int sbuf) {
     constexpr int NH = decltype(nh_tag)::value;
 #pragma unroll
     for (int ks2 = 0; ks2 < 2 * NH; ++ks2) {
@@ -306,7 +317,7 @@ void lane_attn_kv4_kernel(Kv4Params p) {
 #pragma unroll
           for (int q = 0; q < 4 / DT; ++q) exp_pair(sc, pk, m_use, rs, 8 + ks2 * 4 + dt * (4 / DT) + q);
         } else if (decltype(store_tag)::value && (dt & (DT / 2 - 1)) == 0) {
-          store_piece(g, sbuf, 2 * (ks2 - 2) + dt / (DT / 2));
+          store_piece(g[0], pdst, pf, sbuf, 2 * (ks2 - 2) + dt / (DT / 2));
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -315,7 +326,7 @@ void lane_attn_kv4_kernel(Kv4Params p) {
   };
   // Q K^T of the tile in buffer bq into nxt, with the max and the first half of the
   // exponentials of cur between its MFMAs; then cur's P V.
-  auto hot_tile = [&](const Scores& cur, Scores& nxt, int bq, int bv, const Codes& g, int sbuf) {
+  auto hot_tile = [&](const Scores& cur, Scores& nxt, int bq, int bv, const Codes (&g)[NC], int sbuf) {
     bf16x8 kf[2 * KS], pk[4], vf[2][DT];
     float mx = -INFINITY, m_use = 0.f, alpha = 1.f, rs = 0.f;
 #pragma unroll
@@ -345,7 +356,7 @@ void lane_attn_kv4_kernel(Kv4Params p) {
       __builtin_amdgcn_sched_barrier(0);
     }
     rescale(alpha);
-    pv_product(IntTag<2>{}, IntTag<1>{}, cur, pk, vf, m_use, alpha, rs, bv, 0, g, sbuf);
+    pv_product(IntTag<2>{}, IntTag<TPW == K4_WAVES>{}, cur, pk, vf, m_use, alpha, rs, bv, 0, g, sbuf);
   };
   auto cold_tile = [&](auto nh_tag, const Scores& cur, int bv, int half) {   // softmax and P V alone
     constexpr int NH = decltype(nh_tag)::value;
@@ -360,7 +371,8 @@ void lane_attn_kv4_kernel(Kv4Params p) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) vf[0][dt] = vfrag(bv, 0, dt, half);
     __builtin_amdgcn_sched_barrier(0);
-    pv_product(nh_tag, IntTag<0>{}, cur, pk, vf, m_use, alpha, rs, bv, half, Codes{}, 0);
+    const Codes none[NC] = {};
+    pv_product(nh_tag, IntTag<0>{}, cur, pk, vf, m_use, alpha, rs, bv, half, none, 0);
   };
 
   // This split's tiles: prefix tiles [t0, pe), then the lane tiles that some pair of
@@ -372,12 +384,14 @@ void lane_attn_kv4_kernel(Kv4Params p) {
   const int lt0 = next_visible<K4_KT>(p, wg_vis, max(p.n_pre, t0), t_end);   // first lane tile
   if (t0 < pe) {
     auto third = [](int x) { return x >= 3 ? x - 3 : x; };
-    Codes g;
-    load_codes(g, t0);
-    store_codes(g, 0);
-    load_codes(g, min(t0 + 1, pe - 1));
-    store_codes(g, 1);
-    load_codes(g, min(t0 + 2, pe - 1));
+    Codes g[NC];
+    if (staging) {
+      load_codes(g, t0);
+      store_codes(g, 0);
+      load_codes(g, min(t0 + 1, pe - 1));
+      store_codes(g, 1);
+      load_codes(g, min(t0 + 2, pe - 1));
+    }
     __syncthreads();
     Scores sa, sb;
     if (computing) qk(sa, 0);
@@ -386,8 +400,8 @@ void lane_attn_kv4_kernel(Kv4Params p) {
       // (Past the last tile its codes are stored once more, in a buffer that nobody reads.)
       const int sbuf = third(buf + 2);
       if (computing) hot_tile(cur, nxt, third(buf + 1), buf, g, sbuf);
-      else store_codes(g, sbuf);
-      load_codes(g, min(t + 3, pe - 1));
+      else if (staging) store_codes(g, sbuf);
+      if (staging) load_codes(g, min(t + 3, pe - 1));
       // (__syncthreads would wait for the loads too)
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       ++t;
@@ -405,22 +419,22 @@ void lane_attn_kv4_kernel(Kv4Params p) {
     }
     if (t + 1 < pe) {
       step(sa, sb);
-      if (lt0 < t_end) load_rows(rows, lt0);
+      if (staging && lt0 < t_end) load_rows(rows, lt0);
       last(sb);
     } else {
-      if (lt0 < t_end) load_rows(rows, lt0);
+      if (staging && lt0 < t_end) load_rows(rows, lt0);
       last(sa);
     }
     __syncthreads();
-  } else if (lt0 < t_end) {
+  } else if (staging && lt0 < t_end) {
     load_rows(rows, lt0);
   }
   // Lane tiles, one after another in two buffers.
-  if (lt0 < t_end) store_rows(rows, 0);
+  if (staging && lt0 < t_end) store_rows(rows, 0);
   __syncthreads();
   for (int t = lt0, buf = 0; t < t_end; buf ^= 1) {
     const int tn = next_visible<K4_KT>(p, wg_vis, t + 1, t_end);
-    if (tn < t_end) load_rows(rows, tn);
+    if (staging && tn < t_end) load_rows(rows, tn);
     if (computing) {
       const unsigned long long km = key_mask<K4_KT>(pr.vis, (t - p.n_pre) * K4_KT, p.B, p.R);
       // A half that no pair of the wavefront sees is left out.
@@ -428,15 +442,16 @@ void lane_attn_kv4_kernel(Kv4Params p) {
       Scores sc;
       if (lo && hi) {
         qk(sc, buf);
-        mask(IntTag<2>{}, sc, km);
+        if (__ballot(km != ~0ull)) mask(IntTag<2>{}, sc, km);
         cold_tile(IntTag<2>{}, sc, buf, 0);
       } else if (lo || hi) {
         qk_half(sc, buf, hi);
-        mask(IntTag<1>{}, sc, hi ? km >> 32 : km);
+        const unsigned kh = (unsigned)(hi ? km >> 32 : km);
+        if (__ballot(kh != ~0u)) mask(IntTag<1>{}, sc, kh);
         cold_tile(IntTag<1>{}, sc, buf, hi);
       }
     }
-    if (tn < t_end) store_rows(rows, buf ^ 1);
+    if (staging && tn < t_end) store_rows(rows, buf ^ 1);
     __syncthreads();
     t = tn;
   }
@@ -796,16 +811,17 @@ static hipError_t run_kv4_pass(Kv4Params p, const Kv4Pass& s, void* ws, hipStrea
   p.n_pre = s.n_pre;
   p.n_tiles = s.n_tiles;
   p.n_split = s.n_split;
-  p.tpw = s.tpw;
   p.part_o = static_cast<float*>(ws);
   p.part_ml = p.part_o + (size_t)s.n_split * s.n_rows * p.Hq * D;
   const int q_tiles = (s.n_pairs + 31) / 32;
   if (s.units)
     hipLaunchKernelGGL(lane_attn_kv4_unit_kernel<D>, dim3((unsigned)(q_tiles * p.Hkv), 1, s.n_split), dim3(K4_THREADS), 0,
                        stream, p);
-  else
-    hipLaunchKernelGGL(lane_attn_kv4_kernel<D>, dim3((q_tiles + s.tpw - 1) / s.tpw, p.Hkv, s.n_split), dim3(K4_THREADS),
-                       0, stream, p);
+  else {
+    const dim3 grid((q_tiles + s.tpw - 1) / s.tpw, p.Hkv, s.n_split);
+    if (s.tpw == K4_WAVES) hipLaunchKernelGGL((lane_attn_kv4_kernel<D, 8>), grid, dim3(K4_THREADS), 0, stream, p);
+    else hipLaunchKernelGGL((lane_attn_kv4_kernel<D, 4>), grid, dim3(K4_THREADS), 0, stream, p);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || s.n_split == 1) return e;
   const int nrh = s.n_rows * p.Hq, per = 256 / (D / 4);
