@@ -146,7 +146,7 @@ void lane_attn_kv4_kernel(Kv4Params p) {
   const int r32 = lane & 31, hh = lane >> 5, lgrp = lane >> 4, lg = lane & 15;
   const int x0 = blockIdx.x * 32 * TPW;
   const bool computing = w < TPW && x0 + w * 32 < p.n_pairs;
-  const bool staging = TPW == K4_WAVES || w >= TPW;
+  constexpr bool staging = TPW == K4_WAVES;   // (of the loops below; with four query tiles wavefronts 4 .. 7 have their own)
   const Pair pr = pair_at(p, hk, w < TPW ? x0 + w * 32 + r32 : p.n_pairs);
   const unsigned long long wg_vis = blocks_seen(p, x0, x0 + 32 * TPW);
 
@@ -382,6 +382,39 @@ void lane_attn_kv4_kernel(Kv4Params p) {
   const int pe = min(t_end, p.n_pre);
   i32x4 rows[NL];
   const int lt0 = next_visible<K4_KT>(p, wg_vis, max(p.n_pre, t0), t_end);   // first lane tile
+  if (TPW < K4_WAVES && w >= TPW) {   // stages only: the barriers of the loops below
+    if (t0 < pe) {
+      Codes g[NC];
+      load_codes(g, t0);
+      store_codes(g, 0);
+      load_codes(g, min(t0 + 1, pe - 1));
+      store_codes(g, 1);
+      load_codes(g, min(t0 + 2, pe - 1));
+      __syncthreads();
+      int sbuf = 2;
+      for (int t = t0; t + 1 < pe; ++t) {
+        store_codes(g, sbuf);
+        load_codes(g, min(t + 3, pe - 1));
+        sbuf = sbuf == 2 ? 0 : sbuf + 1;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      }
+      if (lt0 < t_end) load_rows(rows, lt0);
+      __syncthreads();
+    } else if (lt0 < t_end) {
+      load_rows(rows, lt0);
+    }
+    if (lt0 < t_end) store_rows(rows, 0);
+    __syncthreads();
+    for (int t = lt0, buf = 0; t < t_end; buf ^= 1) {
+      t = next_visible<K4_KT>(p, wg_vis, t + 1, t_end);
+      if (t < t_end) {
+        load_rows(rows, t);
+        store_rows(rows, buf ^ 1);
+      }
+      __syncthreads();
+    }
+    return;
+  }
   if (t0 < pe) {
     auto third = [](int x) { return x >= 3 ? x - 3 : x; };
     Codes g[NC];
