@@ -135,9 +135,9 @@ void lane_attn_kv4_kernel(Kv4Params p) {
   constexpr int ST = TPW == K4_WAVES ? K4_THREADS : K4_THREADS / 2;   // staging threads
   constexpr int NL = 2 * K4_KT * SEGS / ST;           // bf16 segments per staging thread of a lane tile
   constexpr int AHEAD = 4;          // K fragments read ahead
-  // Fragments of q kept in LDS: at D = 128 the registers hold all but the last two (with all
-  // of them the compiler spills two, and their reloads wait for every load in flight).
-  constexpr int QL = D == 128 ? 2 : 0, QR = KS - QL;
+  // Fragments of q kept in LDS: at D = 128 the registers hold all but the last few (with all
+  // of them the compiler spills some, and their reloads wait for every load in flight).
+  constexpr int QL = D == 64 ? 0 : TPW == K4_WAVES ? 3 : 2, QR = KS - QL;
   __shared__ __attribute__((aligned(1024))) char lds[6 * TB + QL * K4_WAVES * 1024];   // three buffers of K then V, q
 
   const int hk = blockIdx.y, split = blockIdx.z;
