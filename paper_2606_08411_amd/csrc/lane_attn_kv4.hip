@@ -749,6 +749,210 @@ void lane_attn_kv4_unit_kernel(Kv4Params p) {
   }
 }
 
+// ---------------------------------------------------------------- token kernel
+// At most 16 pairs to a K/V head (a single token of a grouped-query model, a few
+// tokens of another): the unit kernel on 16x16x32 MFMAs, whose scores and sums take
+// half the registers and vector work, with sixteen wavefronts to a workgroup.  Lane
+// (key r, quarter b) takes D/4 elements of a key's row: 16 bytes of codes at D = 128,
+// 1 KB a wavefront; q's fragments follow that order of d.  The scores
+//     S^T = K Q^T: lane (pair, b) has keys 16 t + 4 b + (0..3) of the unit's halves t
+// are the second product's operand as they stand, and V's comes from two transpose
+// reads of those keys' rows.
+constexpr int K4_TW = 16;   // wavefronts
+template <int D>
+__global__ __launch_bounds__(K4_TW * kWave) void lane_attn_kv4_token_kernel(Kv4Params p) {
+  constexpr int EL = D / 4, KS = EL / 8, DT = D / 32, OT = D / 16;
+  constexpr int VROWB = 2 * D + 32;         // bytes of a V row in LDS (4 rows of a transpose read in different banks)
+  constexpr int OSTR = D + 4;               // fp32 per pair of the merge area
+  constexpr int WB = K4_UT * VROWB;
+  constexpr int MB = K4_TW * 16 * (OSTR + 2) * 4;
+  __shared__ __attribute__((aligned(16))) char lds[MB > K4_TW * WB ? MB : K4_TW * WB];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, kb = lane >> 4;
+  const int hk = blockIdx.x, split = blockIdx.z;
+  char* const v_s = lds + w * WB;
+  const Pair pr = pair_at(p, hk, r16);
+  const unsigned long long wg_vis = blocks_seen(p, 0, 16);
+
+  bf16x8 qf[KS];
+  {
+    const uint16_t* qrow = p.q + ((size_t)pr.row * p.Hq + pr.hq) * D + kb * EL;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[s] = pr.ok ? load_bf16x8(qrow + 8 * s) : zero_bf16x8();
+  }
+  f32x4 oacc[OT];
+#pragma unroll
+  for (int d = 0; d < OT; ++d) oacc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = -INFINITY, l_run = 0.f;
+
+  struct Codes {
+    unsigned k[2][KS], v[2][KS], ks[2], vs[2];   // of the unit's two 16-key halves
+  };
+  const size_t vplane = (size_t)p.Hkv * p.cap;
+  auto load_codes = [&](Codes& g, int u) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int key = min(u * K4_UT + 16 * t + r16, p.P - 1);   // (a key past the prefix repeats the last one, with P = 0)
+      const size_t row = (size_t)hk * p.cap + key;
+      const uint8_t* kc = p.codes + row * (D / 2) + kb * (EL / 2);
+      __builtin_memcpy(g.k[t], __builtin_assume_aligned(kc, EL / 2), EL / 2);
+      __builtin_memcpy(g.v[t], __builtin_assume_aligned(kc + vplane * (D / 2), EL / 2), EL / 2);
+      const uint8_t* sc = p.scales + row * DT + kb * EL / 32;
+      g.ks[t] = sc[0];
+      g.vs[t] = sc[vplane * DT];
+    }
+  };
+  f32x4 s[2];
+  auto put_v = [&](int t, int j, bf16x8 v) {
+    *reinterpret_cast<bf16x8*>(v_s + (16 * t + r16) * VROWB + (kb * EL + 8 * j) * 2) = v;
+  };
+  // (The region is this wavefront's own: its LDS operations complete in issue order;
+  // the fences order the compiler alone.)
+  auto fence = []() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+  // The scores s are there and V is in LDS; km: the keys of the unit that the pair sees.
+  auto update = [&](unsigned km) {
+    if (__ballot(km != ~0u)) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[t][r] = (km >> (16 * t + 4 * kb + r)) & 1 ? s[t][r] : -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[t][r]);
+    const float m_tile = quad_max(mx) * p.scale_log2;
+    const float m_new = m_tile > m_run + K4_RESCALE_LOG2 ? m_tile : m_run;
+    const float m_use = m_new == -INFINITY ? 0.f : m_new;   // (no key seen yet: all P are 0)
+    const float alpha = exp2_fast(m_run - m_use);
+    m_run = m_new;
+    float rs = 0.f;
+    bf16x8 pk;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float pe = exp2_fast(fmaf(s[t][r], p.scale_log2, -m_use));
+        rs += pe;
+        pk[4 * t + r] = (__bf16)pe;
+      }
+    l_run = l_run * alpha + quad_sum(rs);
+    if (__ballot(alpha != 1.0f)) {
+#pragma unroll
+      for (int d = 0; d < OT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) oacc[d][r] *= alpha;
+    }
+#pragma unroll
+    for (int d = 0; d < OT; ++d) {
+      const uint16_t* va = reinterpret_cast<const uint16_t*>(v_s + (4 * kb + (r16 >> 2)) * VROWB + (16 * d + 4 * (r16 & 3)) * 2);
+      oacc[d] = mfma16x16x32(cat_bf16x4(lds_read_tr16(va), lds_read_tr16(va + 16 * VROWB / 2)), pk, oacc[d]);
+    }
+  };
+
+  const int u0 = (int)((long long)split * p.n_tiles / p.n_split);
+  const int u_end = (int)((long long)(split + 1) * p.n_tiles / p.n_split);
+  const int pe = min(u_end, p.n_pre);
+  int u = u0 + w;
+  {
+    Codes g;
+    if (u < pe) load_codes(g, u);
+    while (u < pe) {
+      fence();
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const float ksc = mx4_scale(g.ks[t]), vsc = mx4_scale(g.vs[t]);
+#pragma unroll
+        for (int j = 0; j < KS; ++j) {
+          put_v(t, j, mx4_bf16x8(g.v[t][j], vsc));
+          s[t] = mfma16x16x32(mx4_bf16x8(g.k[t][j], ksc), qf[j], s[t]);
+        }
+      }
+      fence();
+      const int left = p.P - u * K4_UT;
+      u += K4_TW;
+      if (u < pe) load_codes(g, u);
+      update(left < K4_UT ? (1u << left) - 1 : ~0u);
+    }
+  }
+  // Lane units.
+  for (; u < u_end; u += K4_TW) {
+    const int row0 = (u - p.n_pre) * K4_UT;
+    const int j0 = row0 / p.B, j1 = (min(row0 + K4_UT, p.R) - 1) / p.B;
+    const unsigned long long upto = j1 >= 63 ? ~0ull : (1ull << (j1 + 1)) - 1;
+    if (!(wg_vis & upto & ~((1ull << j0) - 1))) continue;
+    fence();
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const size_t at = ((size_t)min(row0 + 16 * t + r16, p.R - 1) * p.Hkv + hk) * D + kb * EL;
+      s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < KS; ++j) {
+        put_v(t, j, load_bf16x8(p.v_lane + at + 8 * j));
+        s[t] = mfma16x16x32(load_bf16x8(p.k_lane + at + 8 * j), qf[j], s[t]);
+      }
+    }
+    fence();
+    update((unsigned)key_mask<K4_UT>(pr.vis, row0, p.B, p.R));
+  }
+
+  // Combine the wavefronts' states, in ascending order.
+  __syncthreads();
+  float* o_s = reinterpret_cast<float*>(lds);
+  float* ml_s = o_s + K4_TW * 16 * OSTR;
+#pragma unroll
+  for (int d = 0; d < OT; ++d)
+    *reinterpret_cast<f32x4*>(&o_s[(w * 16 + r16) * OSTR + 16 * d + 4 * kb]) = oacc[d];
+  if (kb == 0) {
+    ml_s[(w * 16 + r16) * 2 + 0] = m_run;
+    ml_s[(w * 16 + r16) * 2 + 1] = l_run;
+  }
+  __syncthreads();
+  constexpr int TPR = D / 4;   // threads per pair: all 16 pairs at once (half the threads at D = 64)
+  const int r = tid / TPR, d0 = (tid % TPR) * 4;
+  if (r >= min(16, p.n_pairs)) return;
+  float mw[K4_TW], M = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < K4_TW; ++i) {
+    mw[i] = ml_s[(i * 16 + r) * 2];
+    M = fmaxf(M, mw[i]);
+  }
+  float L = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < K4_TW; ++i) {
+    const float wgt = mw[i] == -INFINITY ? 0.f : exp2_fast(mw[i] - M);
+    L += ml_s[(i * 16 + r) * 2 + 1] * wgt;
+    const f32x4 a = *reinterpret_cast<const f32x4*>(&o_s[(i * 16 + r) * OSTR + d0]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += a[e] * wgt;
+  }
+  const Pair out_pair = pair_at(p, hk, r);
+  const size_t orow = (size_t)out_pair.row * p.Hq + out_pair.hq;
+  if (p.n_split == 1) {
+    const float inv = 1.0f / L;
+    bf16x4 out;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = (__bf16)(acc[e] * inv);
+    *reinterpret_cast<bf16x4*>(p.o + orow * D + d0) = out;
+    if (p.lse && d0 == 0) p.lse[orow] = (M + log2f(L)) * K4_LN2;
+  } else {
+    const size_t at = (size_t)split * p.n_rows * p.Hq + orow;
+    *reinterpret_cast<f32x4*>(p.part_o + at * D + d0) = acc;
+    if (d0 == 0) {
+      p.part_ml[at * 2] = M;
+      p.part_ml[at * 2 + 1] = L;
+    }
+  }
+}
+
 // Combines the NS key splits of each (row, head): D / 4 lanes each, 4 elements a
 // lane, every split's loads issued at once, summed in ascending order.
 template <int D, int NS>
@@ -789,7 +993,7 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(const float* part_o, con
 // ------------------------------------------------------------------ host
 constexpr int K4_MAX_SPLIT = 32;
 struct Kv4Pass {
-  bool units;        // unit kernel (else the tile kernel)
+  bool token, units;   // token kernel, unit kernel (else the tile kernel)
   int n_rows, n_pairs, n_pre, n_tiles, n_split, tpw;
   size_t ws;
 };
@@ -802,8 +1006,15 @@ static Kv4Pass kv4_pass(int n_rows, int R, int P, int Hq, int Hkv, int D) {
   const long long q_tiles = (s.n_pairs + 31) / 32;
   const int units = (P + K4_UT - 1) / K4_UT + (R + K4_UT - 1) / K4_UT;
   s.n_split = 1;
+  s.token = s.n_pairs <= 16;
   s.units = q_tiles * Hkv <= 256;
-  if (s.units) {
+  if (s.token) {
+    s.n_pre = (P + K4_UT - 1) / K4_UT;
+    s.n_tiles = units;
+    // A round of sixteen units takes ~0.7 us, a split and its merge ~4 (MI355X).
+    if (units > 6 * K4_TW)
+      while (s.n_split < K4_MAX_SPLIT && Hkv * s.n_split * 2 <= 256 && units >= 2 * K4_TW * s.n_split) s.n_split *= 2;
+  } else if (s.units) {
     s.n_pre = (P + K4_UT - 1) / K4_UT;
     s.n_tiles = units;
     while (s.n_split < K4_MAX_SPLIT && q_tiles * Hkv * s.n_split * 2 <= 256 && units >= 4 * K4_WAVES * s.n_split) s.n_split *= 2;
@@ -847,7 +1058,9 @@ static hipError_t run_kv4_pass(Kv4Params p, const Kv4Pass& s, void* ws, hipStrea
   p.part_o = static_cast<float*>(ws);
   p.part_ml = p.part_o + (size_t)s.n_split * s.n_rows * p.Hq * D;
   const int q_tiles = (s.n_pairs + 31) / 32;
-  if (s.units)
+  if (s.token)
+    hipLaunchKernelGGL(lane_attn_kv4_token_kernel<D>, dim3(p.Hkv, 1, s.n_split), dim3(K4_TW * kWave), 0, stream, p);
+  else if (s.units)
     hipLaunchKernelGGL(lane_attn_kv4_unit_kernel<D>, dim3((unsigned)(q_tiles * p.Hkv), 1, s.n_split), dim3(K4_THREADS), 0,
                        stream, p);
   else {

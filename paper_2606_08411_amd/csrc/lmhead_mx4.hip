@@ -45,22 +45,6 @@ struct LmMx4Params {
 // so on) then touch every bank once.
 __device__ __forceinline__ int lm_slot(int c) { return (c & 3) | ((c & 8) ? 12 : 0); }
 
-// Over lanes l, l ^ 16, l ^ 32, l ^ 48; the same value on all four.
-__device__ __forceinline__ float quad_max(float v) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return pair_max32(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
-}
-__device__ __forceinline__ float quad_sum(float v) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return pair_sum32(__uint_as_float(r[0]) + __uint_as_float(r[1]));
-}
-__device__ __forceinline__ int quad_min(int v) {
-  const auto r = __builtin_amdgcn_permlane16_swap((unsigned)v, (unsigned)v, false, false);
-  const int w = min((int)r[0], (int)r[1]);
-  const auto t = __builtin_amdgcn_permlane32_swap((unsigned)w, (unsigned)w, false, false);
-  return min((int)t[0], (int)t[1]);
-}
-
 template <int CBT, int WC, int KS, int DEPTH, bool RAGGED, bool NT>
 __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
   constexpr int COLS = 16 * CBT;
