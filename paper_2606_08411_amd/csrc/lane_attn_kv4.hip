@@ -1048,6 +1048,17 @@ size_t kv4_workspace_bytes(int L, int B, int P, int Hq, int Hkv, int D, int n_re
   return a > b ? a : b;
 }
 
+int al_internal_kv4_plan(int L, int B, int P, int Hq, int Hkv, int D, int n_refresh, int32_t* out) {
+  for (int i = 0; i < 2; ++i) {
+    out[2 * i] = out[2 * i + 1] = -1;
+    if (i ? n_refresh <= 0 : L <= 0) continue;
+    const Kv4Pass s = i ? kv4_pass(n_refresh, 0, P, Hq, Hkv, D) : kv4_pass(L * B, L * B, P, Hq, Hkv, D);
+    out[2 * i] = s.token ? 0 : s.units ? 1 : s.tpw;
+    out[2 * i + 1] = s.n_split;
+  }
+  return 0;
+}
+
 template <int D>
 static hipError_t run_kv4_pass(Kv4Params p, const Kv4Pass& s, void* ws, hipStream_t stream) {
   p.n_rows = s.n_rows;

@@ -68,8 +68,15 @@ hipError_t launch_lane_attn_kv4(const uint16_t* q, const uint16_t* k_lane, const
                                 int Hkv, int D, float scale, const int32_t* refresh_idx, int n_refresh,
                                 const uint16_t* q_ref, const uint16_t* k_ref, const uint16_t* v_ref, uint16_t* o_ref,
                                 float* lse_ref, uint16_t* o, float* lse, void* ws, hipStream_t stream);
+// For tests: {0 token kernel, 1 unit kernel, 4 or 8 query tiles of the tile kernel;
+// key splits} of the lane pass, then of the refresh pass (-1 where there is none).
+extern "C" int al_internal_kv4_plan(int L, int B, int P, int Hq, int Hkv, int D, int n_refresh, int32_t* out);
 
 // ---- LM head on a 4-bit weight
+// For tests: {CBT, WC, KS, vocabulary tiles, column tiles, 0 ragged K, 1 W loaded
+// non-temporally, 2 cached} of a call; the (CBT, WC, KS) built, at most `most`.
+extern "C" int al_internal_lmhead_mx4_plan(int N, int d, int V, int32_t* out);
+extern "C" int al_internal_lmhead_mx4_instances(int32_t* out, int most);
 size_t lmhead_mx4_workspace_bytes(int N, int d, int V);
 size_t lmhead_packed_mx4_bytes(int d, int V);
 hipError_t launch_lmhead_pack_mx4(const uint8_t* codes, const uint8_t* scales, int d, int V, uint8_t* out,

@@ -351,11 +351,29 @@ struct LmMx4Layout {
   int cbt, wc, ks, n_vt, n_nt;
 };
 
-// The cheapest instance: n_nt column tiles, and either whole rounds of workgroups of
-// as many units as there are unit rows, or one round with the units shared out over
-// all compute units.
+// Most workgroups over the vocabulary that a layout may have, and the bytes of the
+// partials under it (column tiles pad N to at most 12 fragments more): grows with N,
+// so that a workspace made for N rows serves every smaller call.
+static int lm_mx4_most_vt(int V) {
+  const int n_u = mx4_units(V);
+  return std::max(std::min(n_u, lm_cu_count()), (n_u + 3) / 4);
+}
+size_t lmhead_mx4_workspace_bytes(int N, int d, int V) {
+  (void)d;
+  if (N <= 0 || V <= 0) return 0;
+  return sizeof(LmPartial) * 16 * (size_t)((N + 15) / 16 + 12) * lm_mx4_most_vt(V);
+}
+
+// The cheapest instance under a cost model: n_nt column tiles, and either whole rounds of
+// workgroups of as many units as there are unit rows, or one round with the units
+// shared out over all compute units.  In us (MI355X): a stage takes 0.25 + 0.16 a
+// column fragment for each wavefront on a SIMD, 0.45 at least, a workgroup 3 more
+// (K split: 5.5), and every further column tile reads W again.  d = 4096: V = 16384, 77
+// rows 26 with K split over two wavefronts, 32 without; V = 152064, 128 rows 149
+// unsplit in one column tile, 171 split in two.
 static LmMx4Layout lm_mx4_layout(int N, int d, int V) {
   const int frags = (N + 15) / 16, n_u = mx4_units(V), n_st = mx4_stages(d), cus = lm_cu_count();
+  const int most = lm_mx4_most_vt(V);
   LmMx4Layout best{};
   double best_t = 1e30;
 #define AL_LM_MX4_TRY(CBT, WC, KS, DEPTH)                                                          \
@@ -367,7 +385,7 @@ static LmMx4Layout lm_mx4_layout(int N, int d, int V) {
     const double stage = std::max(0.45, waves * (0.25 + 0.16 * ((CBT + WC - 1) / WC)));            \
     const double rounds = (double)(((long long)n_vt * n_nt + cus - 1) / cus);                      \
     const double t = rounds * (((n_st + KS - 1) / KS) * stage + 3.0 + (KS > 1 ? 2.5 : 0.0)) * (1 + 0.1 * (n_nt - 1));  \
-    if (t < best_t) {                                                                              \
+    if (n_vt <= most && t < best_t) {                                                              \
       best_t = t;                                                                                  \
       best = LmMx4Layout{CBT, WC, KS, n_vt, n_nt};                                                 \
     }                                                                                              \
@@ -379,10 +397,23 @@ static LmMx4Layout lm_mx4_layout(int N, int d, int V) {
   return best;
 }
 
-size_t lmhead_mx4_workspace_bytes(int N, int d, int V) {
-  if (N <= 0 || V <= 0) return 0;
+int al_internal_lmhead_mx4_plan(int N, int d, int V, int32_t* out) {
   const LmMx4Layout L = lm_mx4_layout(N, d, V);
-  return sizeof(LmPartial) * (size_t)L.n_nt * 16 * L.cbt * L.n_vt;
+  const int32_t v[6] = {L.cbt, L.wc, L.ks, L.n_vt, L.n_nt, d % 128 ? 0 : L.n_nt == 1 ? 1 : 2};
+  std::copy(v, v + 6, out);
+  return 0;
+}
+
+int al_internal_lmhead_mx4_instances(int32_t* out, int most) {
+  int n = 0;
+#define AL_LM_MX4_X(CBT, WC, KS, DEPTH)                \
+  if (n < most) {                                      \
+    const int32_t v[3] = {CBT, WC, KS};                \
+    std::copy(v, v + 3, out + 3 * n++);                \
+  }
+  AL_LM_MX4_INSTANCES(AL_LM_MX4_X)
+#undef AL_LM_MX4_X
+  return n;
 }
 
 template <int CBT, int WC, int KS, int DEPTH>

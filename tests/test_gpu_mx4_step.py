@@ -111,7 +111,7 @@ def test_finished_block_joins_the_prefix():
     assert (np.abs(host_f64(o) - ro) <= bo).all() and (np.abs(host_f64(lse) - rl) <= bl).all()
 
 
-@pytest.mark.parametrize("over", [dict(P=150, refresh_frac=0.1), dict(P=3000, L=1, B=1, tree="linear", d=4096)], ids=["refresh", "splits"])
+@pytest.mark.parametrize("over", [dict(P=150, refresh_frac=0.1), dict(P=6000, L=1, B=1, tree="linear", d=4096)], ids=["refresh", "splits"])
 def test_graph_replays(over):
     """Captured and replayed, with eager steps of another group between the replays."""
     t, other = Step("tiny", 3, **over), Step("tiny", 4, **over)
@@ -137,9 +137,9 @@ def test_graph_replays(over):
 
 def test_two_streams():
     """Two groups on two streams at once, on the binding's workspaces."""
-    over = dict(P=3000, L=2, B=3, tree="fork", d=2048, V=3000)
+    over = dict(P=6000, L=2, B=3, tree="fork", d=2048, V=3000)
     steps = [Step("tiny", i, **over) for i in (1, 2)]
-    assert al.lane_attn_kv4_workspace_size(2, 3, 3000, 4, 4, 64) > 0
+    assert al.lane_attn_kv4_workspace_size(2, 3, 6000, 4, 4, 64) > 0
     for t in steps:
         t.run(own_workspaces=False)
     torch.cuda.synchronize()
