@@ -585,25 +585,19 @@ void lane_attn_kv4_unit_kernel(Kv4Params p) {
       g.vs = reinterpret_cast<const uint16_t*>(p.scales)[vplane + row];
     }
   };
-  // A unit: K's and V's operands of this lane's key, the keys its pair sees.
-  auto compute = [&](const bf16x8 (&kf)[KS], const bf16x8 (&vf)[KS], unsigned km) {
-    // The region is this wavefront's own: its LDS operations complete in issue
-    // order; the fences order the compiler alone.
+  // V's row of this lane's key, piece c, j.  (The 16-byte segments of rows 4 .. 7 of
+  // every eight change places in pairs: rows r and r + 4 start in the same bank.)
+  auto put_v = [&](int c, int j, bf16x8 v) {
+    *reinterpret_cast<bf16x8*>(&v_s[r32 * VROW + 64 * c + 32 * hh + 8 * (j ^ ((r32 >> 2) & 1))]) = v;
+  };
+  // (The region is this wavefront's own: its LDS operations complete in issue order;
+  // the fences order the compiler alone.)
+  auto fence = []() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-#pragma unroll
-    for (int i = 0; i < KS; ++i)
-      *reinterpret_cast<bf16x8*>(&v_s[r32 * VROW + 64 * (i >> 2) + 32 * hh + 8 * (i & 3)]) = vf[i];
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    f32x16 s = {}, s1 = {};
-#pragma unroll
-    for (int i = 0; i < KS; i += 2) {
-      s = mfma32x32x16(kf[i], qf[i], s);
-      s1 = mfma32x32x16(kf[i + 1], qf[i + 1], s1);
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] += s1[r];
+  };
+  // A unit's scores are there and V is in LDS; km: the keys that the pair sees.
+  auto update = [&](f32x16 s, unsigned km) {
     if (__ballot(km != ~0u)) {
       const unsigned mw = km >> (4 * hh);
 #pragma unroll
@@ -636,7 +630,7 @@ void lane_attn_kv4_unit_kernel(Kv4Params p) {
     for (int ks2 = 0; ks2 < 2; ++ks2)
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        const uint16_t* va = &v_s[(16 * ks2 + 4 * hh + (lg >> 2)) * VROW + dt * 32 + 16 * (lgrp & 1) + 4 * (lg & 3)];
+        const uint16_t* va = &v_s[(16 * ks2 + 4 * hh + (lg >> 2)) * VROW + dt * 32 + 16 * (lgrp & 1) + 4 * ((lg & 3) ^ (2 * hh))];
         oacc[dt] = mfma32x32x16(cat_bf16x4(lds_read_tr16(va), lds_read_tr16(va + 8 * VROW)), pk[ks2], oacc[dt]);
       }
   };
@@ -654,30 +648,13 @@ void lane_attn_kv4_unit_kernel(Kv4Params p) {
     }
     return u;
   };
+  // The lane units come first: their rows arrive while q does.
+  const int pe = min(u_end, p.n_pre);
   int u = u0 + w;
-  {
-    Codes g;
-    const int pe = min(u_end, p.n_pre);
-    if (u < pe) load_codes(g, u);
-    while (u < pe) {
-      bf16x8 kf[KS], vf[KS];
-#pragma unroll
-      for (int c = 0; c < DC; ++c) {
-        const float ksc = mx4_scale((g.ks >> (16 * c + 8 * hh)) & 255), vsc = mx4_scale((g.vs >> (16 * c + 8 * hh)) & 255);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          kf[4 * c + j] = mx4_bf16x8((unsigned)g.x[c][j], ksc);
-          vf[4 * c + j] = mx4_bf16x8((unsigned)g.x[DC + c][j], vsc);
-        }
-      }
-      const int left = p.P - u * K4_UT;
-      u += K4_WAVES;
-      if (u < pe) load_codes(g, u);
-      compute(kf, vf, left < K4_UT ? (1u << left) - 1 : ~0u);
-    }
-  }
-  for (u = seen(u); u < u_end; u = seen(u + K4_WAVES)) {
-    const int r = min((u - p.n_pre) * K4_UT + r32, p.R - 1);
+  Codes g;
+  if (u < pe) load_codes(g, u);
+  for (int v = seen(u < p.n_pre ? u + (p.n_pre - u + K4_WAVES - 1) / K4_WAVES * K4_WAVES : u); v < u_end; v = seen(v + K4_WAVES)) {
+    const int r = min((v - p.n_pre) * K4_UT + r32, p.R - 1);
     const size_t at = ((size_t)r * p.Hkv + hk) * D + 32 * hh;
     bf16x8 kf[KS], vf[KS];
 #pragma unroll
@@ -685,7 +662,34 @@ void lane_attn_kv4_unit_kernel(Kv4Params p) {
       kf[i] = load_bf16x8(p.k_lane + at + 64 * (i >> 2) + 8 * (i & 3));
       vf[i] = load_bf16x8(p.v_lane + at + 64 * (i >> 2) + 8 * (i & 3));
     }
-    compute(kf, vf, (unsigned)key_mask<K4_UT>(pr.vis, (u - p.n_pre) * K4_UT, p.B, p.R));
+    const unsigned km = (unsigned)key_mask<K4_UT>(pr.vis, (v - p.n_pre) * K4_UT, p.B, p.R);
+    fence();
+    f32x16 s = {};
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      put_v(i >> 2, i & 3, vf[i]);
+      s = mfma32x32x16(kf[i], qf[i], s);
+    }
+    fence();
+    update(s, km);
+  }
+  while (u < pe) {
+    fence();
+    f32x16 s = {};
+#pragma unroll
+    for (int c = 0; c < DC; ++c) {
+      const float ksc = mx4_scale((g.ks >> (16 * c + 8 * hh)) & 255), vsc = mx4_scale((g.vs >> (16 * c + 8 * hh)) & 255);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        put_v(c, j, mx4_bf16x8((unsigned)g.x[DC + c][j], vsc));
+        s = mfma32x32x16(mx4_bf16x8((unsigned)g.x[c][j], ksc), qf[4 * c + j], s);
+      }
+    }
+    fence();
+    const int left = p.P - u * K4_UT;
+    u += K4_WAVES;
+    if (u < pe) load_codes(g, u);
+    update(s, left < K4_UT ? (1u << left) - 1 : ~0u);
   }
 
   // Combine the wavefronts' states, in ascending order.
