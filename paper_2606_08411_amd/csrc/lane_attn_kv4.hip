@@ -957,35 +957,64 @@ __global__ __launch_bounds__(K4_TW * kWave) void lane_attn_kv4_token_kernel(Kv4P
   }
 }
 
-// Combines the NS key splits of each (row, head): D / 4 lanes each, 4 elements a
-// lane, every split's loads issued at once, summed in ascending order.
+// Combines the NS key splits of each (row, head): D / 4 lanes to a run of K4_RUN
+// splits, 4 elements a lane, all loads of a run issued at once; then the runs through
+// LDS.  Both sums go in ascending order.  (All splits in one run: 32 of them fill the
+// registers; a call over 8192 rows 16.4 us, 14.7 with runs of 8.)
+constexpr int K4_RUN = 8;
 template <int D, int NS>
 __global__ __launch_bounds__(256) void kv4_merge_kernel(const float* part_o, const float* part_ml, int n_rowheads,
                                                         uint16_t* o, float* lse) {
-  constexpr int LPR = D / 4;
-  const int rh = blockIdx.x * (256 / LPR) + threadIdx.x / LPR, sl = threadIdx.x % LPR;
-  if (rh >= n_rowheads) return;
-  float m[NS], l[NS];
-  f32x4 v[NS];
+  constexpr int LPR = D / 4, N = NS < K4_RUN ? NS : K4_RUN, RUNS = NS / N, PER = 256 / LPR / RUNS;
+  static_assert(PER >= 1, "a row's runs are one workgroup's");
+  const int sl = threadIdx.x % LPR, run = threadIdx.x / LPR % RUNS;
+  const int rh = blockIdx.x * PER + threadIdx.x / (LPR * RUNS), rc = min(rh, n_rowheads - 1);
+  float m[N], l[N];
+  f32x4 v[N];
 #pragma unroll
-  for (int s = 0; s < NS; ++s) {
-    const float2 ml = *reinterpret_cast<const float2*>(part_ml + ((size_t)s * n_rowheads + rh) * 2);
+  for (int s = 0; s < N; ++s) {
+    const size_t at = (size_t)(run * N + s) * n_rowheads + rc;
+    const float2 ml = *reinterpret_cast<const float2*>(part_ml + at * 2);
     m[s] = ml.x;
     l[s] = ml.y;
-    v[s] = *reinterpret_cast<const f32x4*>(part_o + ((size_t)s * n_rowheads + rh) * D + sl * 4);
+    v[s] = *reinterpret_cast<const f32x4*>(part_o + at * D + sl * 4);
   }
-  float M = -INFINITY;
-#pragma unroll
-  for (int s = 0; s < NS; ++s) M = fmaxf(M, m[s]);
-  float L = 0.f;
+  float M = -INFINITY, L = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int s = 0; s < NS; ++s) {
-    const float wgt = exp2_fast(m[s] - M);   // (0 where the split saw no key; M is finite)
-    L += l[s] * wgt;
+  for (int s = 0; s < N; ++s) M = fmaxf(M, m[s]);
+  {
+    const float ref = M == -INFINITY ? 0.f : M;   // (no split of the run saw a key: weights 0)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] += v[s][e] * wgt;
+    for (int s = 0; s < N; ++s) {
+      const float wgt = exp2_fast(m[s] - ref);
+      L += l[s] * wgt;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += v[s][e] * wgt;
+    }
   }
+  if constexpr (RUNS > 1) {
+    __shared__ f32x4 acc_s[256];
+    __shared__ float2 ml_s[256];
+    acc_s[threadIdx.x] = acc;
+    ml_s[threadIdx.x] = float2{M, L};
+    __syncthreads();
+    if (run) return;
+#pragma unroll
+    for (int s = 1; s < RUNS; ++s) M = fmaxf(M, ml_s[threadIdx.x + s * LPR].x);   // (some run saw a key: finite)
+    L = 0.f;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < RUNS; ++s) {
+      const float2 ml = ml_s[threadIdx.x + s * LPR];
+      const f32x4 a = acc_s[threadIdx.x + s * LPR];
+      const float wgt = exp2_fast(ml.x - M);
+      L += ml.y * wgt;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += a[e] * wgt;
+    }
+  }
+  if (rh >= n_rowheads) return;
   const float inv = 1.0f / L;
   bf16x4 out;
 #pragma unroll
@@ -994,8 +1023,14 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(const float* part_o, con
   if (lse && sl == 0) lse[rh] = (M + log2f(L)) * K4_LN2;
 }
 
+template <int D, int NS>
+static void launch_kv4_merge(const float* part_o, const float* part_ml, int n, uint16_t* o, float* lse, hipStream_t stream) {
+  constexpr int runs = NS < K4_RUN ? 1 : NS / K4_RUN, per = 256 / (D / 4) / runs;
+  hipLaunchKernelGGL((kv4_merge_kernel<D, NS>), dim3((n + per - 1) / per), dim3(256), 0, stream, part_o, part_ml, n, o, lse);
+}
+
 // ------------------------------------------------------------------ host
-constexpr int K4_MAX_SPLIT = 32;
+constexpr int K4_MAX_SPLIT = 64;
 struct Kv4Pass {
   bool token, units;   // token kernel, unit kernel (else the tile kernel)
   int n_rows, n_pairs, n_pre, n_tiles, n_split, tpw;
@@ -1015,8 +1050,10 @@ static Kv4Pass kv4_pass(int n_rows, int R, int P, int Hq, int Hkv, int D) {
   if (s.token) {
     s.n_pre = (P + K4_UT - 1) / K4_UT;
     s.n_tiles = units;
-    // A round of sixteen units takes ~0.7 us, a split and its merge ~4 (MI355X).
-    if (units > 6 * K4_TW)
+    // One token, 28 heads on 4: 1024 rows 9.7 us unsplit, 11.3 with two splits; 2048 rows 12.7 and
+    // 11.4, 3000 rows 15.9 and 11.3 with four (MI355X).  64 splits against 32 (half of the
+    // compute units): 32769 rows 14 -> 11.5, 131072 rows 23.8 -> 18.7.
+    if (units > 3 * K4_TW)
       while (s.n_split < K4_MAX_SPLIT && Hkv * s.n_split * 2 <= 256 && units >= 2 * K4_TW * s.n_split) s.n_split *= 2;
   } else if (s.units) {
     s.n_pre = (P + K4_UT - 1) / K4_UT;
@@ -1085,14 +1122,11 @@ static hipError_t run_kv4_pass(Kv4Params p, const Kv4Pass& s, void* ws, hipStrea
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || s.n_split == 1) return e;
-  const int nrh = s.n_rows * p.Hq, per = 256 / (D / 4);
-  const dim3 grid((nrh + per - 1) / per);
-#define AL_K4_MERGE(NS)                                                                                    \
-  case NS:                                                                                                 \
-    hipLaunchKernelGGL((kv4_merge_kernel<D, NS>), grid, dim3(256), 0, stream, p.part_o, p.part_ml, nrh, p.o, p.lse); \
-    break;
+  const int nrh = s.n_rows * p.Hq;
+#define AL_K4_MERGE(NS) \
+  case NS: launch_kv4_merge<D, NS>(p.part_o, p.part_ml, nrh, p.o, p.lse, stream); break;
   switch (s.n_split) {
-    AL_K4_MERGE(2) AL_K4_MERGE(4) AL_K4_MERGE(8) AL_K4_MERGE(16) AL_K4_MERGE(32)
+    AL_K4_MERGE(2) AL_K4_MERGE(4) AL_K4_MERGE(8) AL_K4_MERGE(16) AL_K4_MERGE(32) AL_K4_MERGE(64)
     default: return hipErrorInvalidValue;
   }
 #undef AL_K4_MERGE

@@ -64,6 +64,8 @@ ATTN_CASES = [  # L, B, P, Hq, Hkv, D, refreshed rows
     (0, 1, 1299, 7, 1, 64, 1299), (0, 1, 2061, 8, 8, 64, 2061), (0, 1, 1108, 8, 2, 128, 1108), (0, 1, 1098, 8, 8, 128, 1098),
     (33, 16, 5326, 32, 2, 64, 0), (33, 64, 6960, 8, 2, 64, 1), (33, 16, 8968, 32, 8, 128, 0), (33, 100, 7597, 7, 1, 128, 1),
     (2, 100, 20675, 56, 8, 128, 0), (5, 64, 23356, 32, 32, 64, 0), (33, 16, 18507, 16, 4, 64, 0), (33, 64, 16255, 4, 4, 128, 0),
+    (1, 1, 1800, 1, 1, 64, 0), (1, 1, 1810, 28, 4, 128, 0), (1, 1, 33001, 2, 2, 64, 0), (1, 32, 33005, 1, 1, 128, 0),
+    (1, 3, 33003, 8, 2, 64, 0),
 ]
 
 
