@@ -9,8 +9,11 @@
 // lane 16 b + r of a wavefront takes the 16 bytes of row r, scale block b, so one
 // dwordx4 load per 16 rows and stage, one scale per lane and four MFMA steps of 8
 // elements a lane (a contraction may walk its index in any order, as long as both
-// operands do).  W goes straight to registers, two stages ahead: no wavefront
-// of the same column needs another's, and LDS carries only the hidden rows.
+// operands do).  W goes straight to registers, two or three stages ahead: no wavefront
+// of the same column needs another's, and LDS carries only the hidden rows.  A
+// stage's loads are issued one to each group of MFMAs: all at its start they keep the
+// wavefronts from the matrix cores while the address unit takes them (8 wavefronts x up
+// to 12 KB at 64 bytes a cycle; 614 rows of the 126464 x 4096 head 500 us, 470 spread).
 //
 // What bounds it: with few columns the W stream (17/32 byte an element, against
 // 2 in bf16), with many the matrix cores.  A stage of a wavefront is 64
@@ -65,44 +68,50 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
   const bool active = u < u_end;   // (a wavefront past the tile's units loads hidden rows only)
 
   // Hidden rows go straight to LDS, in pieces of 1 KB (4 rows of a stage): pieces w + 8
-  // i of a group of KS stages by wavefront w (the last one again where there are
-  // none left, so that every wavefront has LH loads a group).  Elements past d are
-  // zero.  (Stages past the last load from the first: the loads of a group are
-  // always the same number and need no branch, so every wait counts them exactly.)
+  // i of a group of KS stages by wavefront w (an earlier one with the same rows mod 16
+  // again where there are none left, so that every wavefront has LH loads a group).
+  // Past d, where the packed W is zero, a segment of the same row is read again.
+  // (Stages past the last load from the first: the loads of a group are always the
+  // same number and need no branch, so every wait counts them exactly.)
   const unsigned ring0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
   unsigned hoff[LH];   // bytes (n_rows * d < 2^31)
-  auto piece = [&](int i) { return min(w + LM_MX4_WAVES * i, KS * COLS / 4 - 1); };
+  auto piece = [&](int i) {
+    const int q = w + LM_MX4_WAVES * i;
+    return q < KS * COLS / 4 ? q : q - (i ? LM_MX4_WAVES : 4);
+  };
+  const int hseg = l16 ^ lm_slot((4 * w + kb) & 15);   // this lane's segment of a stage, in every piece
 #pragma unroll
   for (int i = 0; i < LH; ++i) {
     const int c = 4 * (piece(i) % (COLS / 4)) + kb;
     const int n = min(nt * COLS + c, p.N - 1);
-    hoff[i] = 2 * (unsigned)(p.row_idx ? p.row_idx[n] : n) * (unsigned)p.d + (l16 ^ lm_slot(c & 15)) * 16;
+    hoff[i] = 2 * (unsigned)(p.row_idx ? p.row_idx[n] : n) * (unsigned)p.d + hseg * 16;
   }
+  auto load_hidden1 = [&](int group, int slot, int i) {
+    const int st = group * KS + piece(i) / (COLS / 4);
+    const char* src = reinterpret_cast<const char*>(p.hidden) + (size_t)(st < p.n_st ? st : 0) * 256;
+    const unsigned lds_at = ring0 + slot + piece(i) * 1024;
+    unsigned off = hoff[i];
+    if (RAGGED) off -= st * 128 + 8 * hseg < p.d ? 0 : 16 * hseg;
+    load_to_lds16<0, 0, false>(uniform_ptr(src), off, lds_at);
+  };
   auto load_hidden = [&](int group, int slot) {
 #pragma unroll
-    for (int i = 0; i < LH; ++i) {
-      const int st = group * KS + piece(i) / (COLS / 4);
-      const char* src = reinterpret_cast<const char*>(p.hidden) + (size_t)(st < p.n_st ? st : 0) * 256;
-      const unsigned lds_at = ring0 + slot + piece(i) * 1024;
-      if (RAGGED) {
-        const int k = st * 128 + (l16 ^ lm_slot((4 * piece(i) + kb) & 15)) * 8;
-        load_to_lds16<0>(k < p.d ? src + hoff[i] : reinterpret_cast<const char*>(zero_seg16), lds_at);
-      } else {
-        load_to_lds16<0, 0, false>(uniform_ptr(src), hoff[i], lds_at);
-      }
-    }
+    for (int i = 0; i < LH; ++i) load_hidden1(group, slot, i);
   };
   struct Stage {
     i32x4 c[4];
     unsigned s;
   };
-  auto load_w = [&](Stage& g, int st) {
+  auto load_w1 = [&](Stage& g, int st, int i) {   // i = 0..3: codes, 4: scales
     const int in = st < p.n_st;
     const size_t at = (size_t)(in ? st : 0) * p.n_u + (in ? u : 0);
     const i32x4* src = reinterpret_cast<const i32x4*>(p.codes) + at * 256 + lane;
+    if (i < 4) g.c[i] = NT ? __builtin_nontemporal_load(src + i * 64) : src[i * 64];
+    else g.s = reinterpret_cast<const unsigned*>(p.scales)[at * 64 + lane];
+  };
+  auto load_w = [&](Stage& g, int st) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) g.c[i] = NT ? __builtin_nontemporal_load(src + i * 64) : src[i * 64];
-    g.s = reinterpret_cast<const unsigned*>(p.scales)[at * 64 + lane];
+    for (int i = 0; i < 5; ++i) load_w1(g, st, i);
   };
 
   auto body = [&](auto nc_tag) {
@@ -119,40 +128,39 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
     constexpr bool ROLL = CBT > 10;
     constexpr int RPG = (NC + 3) / 4, NB = ROLL ? 1 : 2;
     const int brow = (wc * CB0 * 16 + l16) * 256;
-    auto compute = [&](const Stage& g, int slot) {
-      const char* b0 = ring + slot + brow;
-      bf16x8 b[NB][NC], a[2];
-      auto read_b = [&](int s, int j) {
-        b[s % NB][j] = *reinterpret_cast<const bf16x8*>(b0 + j * 4096 + (((4 * kb + s) ^ lm_slot(l16)) * 16));
-      };
-      auto convert = [&](int q) {   // group q = 4 s + i
-        a[q & 1] = mx4_bf16x8((unsigned)g.c[q & 3][q >> 2], mx4_scale((g.s >> (8 * (q & 3))) & 255));
-      };
-#pragma unroll
-      for (int j = 0; j < NC; ++j) read_b(0, j);
-      convert(0);
+    bf16x8 b[NB][NC], a[2];
+    auto read_b = [&](int slot, int s, int j) {
+      b[s % NB][j] = *reinterpret_cast<const bf16x8*>(ring + slot + brow + j * 4096 + (((4 * kb + s) ^ lm_slot(l16)) * 16));
+    };
+    auto convert = [&](const Stage& g, int q) {   // group q = 4 s + i
+      a[q & 1] = mx4_bf16x8((unsigned)g.c[q & 3][q >> 2], mx4_scale((g.s >> (8 * (q & 3))) & 255));
+    };
+    // (The next stage's first fragments come with this one's last step: its hidden rows
+    // are in LDS already, and the matrix cores need not wait for them behind the barrier.)
+    auto compute = [&](const Stage& g, int slot, const Stage& gn, int slot_n, auto load) {
 #pragma unroll
       for (int q = 0; q < 16; ++q) {
         const int s = q >> 2, i = q & 3;
-        if (s < 3 && !ROLL) {
+        load(q);
+        if (!ROLL) {
 #pragma unroll
           for (int j = i * RPG; j < (i + 1) * RPG; ++j)
-            if (j < NC) read_b(s + 1, j);
+            if (j < NC) read_b(s < 3 ? slot : slot_n, (s + 1) & 3, j);
         }
-        if (q < 15) convert(q + 1);
+        if (q < 15) convert(g, q + 1);
+        else convert(gn, 0);
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
           acc[i][j] = mfma16x16x32(a[q & 1], b[s % NB][j], acc[i][j]);
-          if (ROLL && s < 3 && i == 3) read_b(s + 1, j);
+          if (ROLL && i == 3) read_b(s < 3 ? slot : slot_n, (s + 1) & 3, j);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
     };
     // Group i is stages KS i .. KS i + KS - 1, of which this wavefront multiplies stage
-    // KS i + ks.  At the barrier on its top the group's hidden rows have arrived (all
-    // but the loads issued after them: W twice and one group of hidden rows),
-    // everyone is done with the group before, and its buffer takes the hidden rows
-    // of the group after next.
+    // KS i + ks.  At the barrier on its top the hidden rows of groups i and i + 1 have
+    // arrived (all but the five loads of W issued after them), everyone is done with
+    // group i - 1, and its buffer takes the hidden rows of group i + 2.
     const int n_group = (p.n_st + KS - 1) / KS;
     int slot = 0;   // byte of the ring
     auto next_slot = [&](int x, int by) {
@@ -162,8 +170,9 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
     if (!active) {
       load_hidden(0, 0);
       load_hidden(1, KS * HB);
+      wait_loads_and_barrier<0>();
       for (int i = 0; i < n_group; ++i) {
-        wait_loads_and_barrier<LH>();
+        if (i) wait_loads_and_barrier<0>();
         load_hidden(i + 2, next_slot(slot, 2));
         slot = next_slot(slot, 1);
       }
@@ -176,18 +185,23 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
       }
       load_hidden(0, 0);
       load_hidden(1, KS * HB);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      wait_loads_and_barrier<0>();
+#pragma unroll
+      for (int j = 0; j < NC; ++j) read_b(ks * HB, 0, j);
+      convert(g[0], 0);
       // (One group inside the other's condition: no path leaves one out and takes a
       // later one, so the compiler's waits for W stay exact too.)
       auto step = [&](auto self, auto q_tag, int i0) -> void {
         constexpr int q = decltype(q_tag)::value;
         const int i = i0 + q;
         if (i < n_group) {
-          wait_loads_and_barrier<10 + LH>();
-          load_hidden(i + 2, next_slot(slot, 2));
-          load_w(g[(q + DEPTH - 1) % DEPTH], (i + DEPTH - 1) * KS + ks);
-          __builtin_amdgcn_sched_barrier(0);
-          if (KS == 1 || i * KS + ks < p.n_st) compute(g[q], slot + ks * HB);
+          if (q > 0 || i0 > 0) wait_loads_and_barrier<5>();
+          const int slot2 = next_slot(slot, 2);
+          auto load = [&](int t) {
+            if (t < LH) load_hidden1(i + 2, slot2, t);
+            else if (t < LH + 5) load_w1(g[(q + DEPTH - 1) % DEPTH], (i + DEPTH - 1) * KS + ks, t - LH);
+          };
+          if (KS == 1 || i * KS + ks < p.n_st) compute(g[q], slot + ks * HB, g[(q + 1) % DEPTH], next_slot(slot, 1) + ks * HB, load);
           slot = next_slot(slot, 1);
           if constexpr (q + 1 < DEPTH) self(self, IntTag<q + 1>{}, i0);
         }
