@@ -12,11 +12,13 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/EmptyTensor.h>
 #include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
 #include <cstdint>
+#include <optional>
 #include <vector>
 
 #include "../../include/asynclane.h"
@@ -197,6 +199,17 @@ bool status_ok(int st, const char* what) {
   return false;
 }
 
+// A new output beside `like`, from the allocator of its storage.  (at::empty finds the
+// same allocator through the dispatcher, 0.3-0.5 us a tensor; a storage without one goes
+// that way.)
+at::Tensor fresh(const at::Tensor& like, at::IntArrayRef size, at::ScalarType type) {
+  if (c10::Allocator* const from = like.storage().allocator()) {
+    at::Tensor t(at::detail::empty_generic(size, from, c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt));
+    if (t.device() == like.device()) return t;
+  }
+  return at::empty(size, like.options().dtype(type));
+}
+
 PyObject* decline() { Py_RETURN_NONE; }
 
 template <class F>
@@ -357,17 +370,16 @@ PyObject* lmhead(PyObject*, PyObject* const* a, Py_ssize_t na) {
     void* ws = g.ok ? workspace(g, a[10], MX4 ? "lmhead_mx4" : "lmhead", need, *h, dev, stream, &bytes, keep) : nullptr;
     if (!g.ok) return decline();
     at::Tensor mc, ma, ml;
-    const auto f32 = h->options().dtype(at::kFloat);
     if (!conf) {
-      mc = at::empty({N}, f32);
+      mc = fresh(*h, {N}, at::kFloat);
       cp = mc.data_ptr();
     }
     if (!arg) {
-      ma = at::empty({N}, h->options().dtype(at::kInt));
+      ma = fresh(*h, {N}, at::kInt);
       ap = ma.data_ptr();
     }
     if (!lse && want) {
-      ml = at::empty({N}, f32);
+      ml = fresh(*h, {N}, at::kFloat);
       lp = ml.data_ptr();
     }
     int st;
@@ -476,19 +488,19 @@ PyObject* attn_kv4(PyObject*, PyObject* const* a, Py_ssize_t na) {
     void* ws = g.ok ? workspace(g, a[18], "attn_kv4", need, *kc, dev, stream, &bytes, keep) : nullptr;
     if (!g.ok) return decline();
     if (L > 0 && !o) {
-      mo = at::empty({L * B, Hq, kv.D}, q->options());
+      mo = fresh(*q, {L * B, Hq, kv.D}, at::kBFloat16);
       op = mo.data_ptr();
     }
     if (L > 0 && !lse && want) {
-      ml = at::empty({L * B, Hq}, kc->options().dtype(f32));
+      ml = fresh(*kc, {L * B, Hq}, at::kFloat);
       lp = ml.data_ptr();
     }
     if (n_ref && !o_r) {
-      mor = at::empty({n_ref, Hq, kv.D}, qr->options());
+      mor = fresh(*qr, {n_ref, Hq, kv.D}, at::kBFloat16);
       orp = mor.data_ptr();
     }
     if (n_ref && !lse_r && want) {
-      mlr = at::empty({n_ref, Hq}, kc->options().dtype(f32));
+      mlr = fresh(*kc, {n_ref, Hq}, at::kFloat);
       lrp = mlr.data_ptr();
     }
     int st;
@@ -535,11 +547,11 @@ PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t na) {
     if (!g.ok) return decline();
     at::Tensor mc, ms;
     if (!c) {
-      mc = at::empty(with_last(*x, n / 2), x->options().dtype(at::kByte));
+      mc = fresh(*x, with_last(*x, n / 2), at::kByte);
       cp = mc.data_ptr();
     }
     if (!s) {
-      ms = at::empty(with_last(*x, n / 32), x->options().dtype(at::kByte));
+      ms = fresh(*x, with_last(*x, n / 32), at::kByte);
       sp = ms.data_ptr();
     }
     int st;
@@ -571,7 +583,7 @@ PyObject* dequantize(PyObject*, PyObject* const* a, Py_ssize_t na) {
     if (!g.ok) return decline();
     at::Tensor my;
     if (!y) {
-      my = at::empty(with_last(*c, n), c->options().dtype(at::kBFloat16));
+      my = fresh(*c, with_last(*c, n), at::kBFloat16);
       yp = my.data_ptr();
     }
     int st;

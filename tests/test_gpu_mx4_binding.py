@@ -156,3 +156,33 @@ def test_a_capture_needs_a_workspace():
     with pytest.raises(al.AsyncLaneError, match="pass workspace="):
         with torch.cuda.graph(graph):
             al.lmhead_confidence_mx4(**a)
+
+
+def test_outputs_are_ordinary_tensors():
+    """New outputs: of the caching allocator, on the input's device, inference tensors where inputs would be;
+    also beside an input whose storage has no allocator."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    x = torch.randn((3, 64, 256), generator=g, device="cuda").bfloat16()
+    codes, scales = al.mx4_quantize(x)
+    before = torch.cuda.memory_allocated()
+    c, s = al.mx4_quantize(x)
+    y = al.mx4_dequantize(c, s)
+    assert torch.cuda.memory_allocated() - before >= c.nbytes + s.nbytes + y.nbytes
+    for t, shape, dtype in ((c, (3, 64, 128), torch.uint8), (s, (3, 64, 8), torch.uint8), (y, (3, 64, 256), torch.bfloat16)):
+        assert t.shape == shape and t.dtype == dtype and t.device == x.device
+        assert t.is_contiguous() and t.is_leaf and not t.requires_grad and not t.is_inference()
+    y.requires_grad_()
+    (y.float() ** 2).sum().backward()
+    assert torch.equal(y.grad, (2 * y.detach().float()).bfloat16())
+    with torch.inference_mode():
+        assert all(t.is_inference() for t in al.mx4_quantize(x))
+    shared = torch.utils.dlpack.from_dlpack(torch.utils.dlpack.to_dlpack(x))
+    for t, want in zip(al.mx4_quantize(shared), (codes, scales)):
+        assert torch.equal(t, want)
+    W = al.lmhead_pack_weight_mx4(*al.mx4_quantize(x[0]))
+    conf, arg, lse = al.lmhead_confidence_mx4(x[1], W, 64)
+    assert conf.dtype == lse.dtype == torch.float32 and arg.dtype == torch.int32
+    assert conf.shape == arg.shape == lse.shape == (64,)
+    del c, s, y
+    torch.cuda.synchronize()
