@@ -171,10 +171,10 @@ void lane_attn_kv4_kernel(Kv4Params p) {
 
   // Staging.  Row r's 16-byte segment s sits in slot s ^ f(r): f_K puts the 16 rows
   // that one LDS cycle of the K reads serves into different banks, f_V the rows of
-  // a transpose read.
+  // a transpose read; f_V's low bit parts the neighbouring rows of a store.
   auto fk = [](int r) { return D == 128 ? r & 15 : (r >> 1) & 7; };
   auto fv = [](int r) {
-    return D == 128 ? (4 * (r & 3)) ^ (2 * ((r >> 2) & 1)) : (4 * ((r >> 1) & 1)) ^ (2 * ((r >> 2) & 1));
+    return D == 128 ? (4 * (r & 3)) ^ (2 * ((r >> 2) & 1)) ^ (r & 1) : (5 * ((r >> 1) & 1)) ^ (2 * ((r >> 2) & 1));
   };
   struct Codes {      // of a prefix tile: 32 elements
     i32x4 x;
