@@ -9,11 +9,12 @@
 // blocks a pair sees is a mask of its own lane of the wavefront (S^T = K Q^T
 // leaves a pair's scores to the wavefront lanes l and l ^ 32).
 //
-// Keys.  Tiles of 64: first the prefix, then the rows of all lane blocks as one
-// list.  A prefix tile is read as codes (a 16-byte load per 32 elements), converted
-// to bf16 (exact) and written to LDS once per workgroup, K and V row-major with
-// their 16-byte segments permuted; a lane tile is copied.  Both products are the
-// 32x32x16 bf16 MFMA with fp32 accumulation, transposed as in lane_attn.hip:
+// Keys.  First the prefix, then the rows of all lane blocks as one list, in tiles of
+// 64 (the tile kernel: many query tiles, which share the converted keys of a
+// workgroup) or units of 32 (the unit kernel: few query tiles, a wavefront to a unit;
+// the token kernel: at most 16 pairs to a K/V head).  Prefix rows are read as codes (a
+// 16-byte load per 32 elements) and converted to bf16, which is exact.  Both products
+// are bf16 MFMAs with fp32 accumulation, transposed as in lane_attn.hip:
 //     S^T = K Q^T,   O^T = V^T P^T  (V^T by LDS transpose reads).
 // P is rounded to bf16 for the second product; the row sum adds the unrounded
 // fp32 values, so the log-sum-exp keeps fp32 accuracy (adding the rounded ones
@@ -21,6 +22,11 @@
 //
 // Keys are split over blockIdx.z where there are few query tiles; the splits'
 // partials are kept in fp32 and combined by kv4_merge_kernel.
+//
+// Per call (MI355X; keys x K/V heads, query heads, rows): the tile kernel 172 us for
+// 2048 rows x 32 heads over 4096 keys and their lane blocks (about 0.85 PFLOP/s),
+// the unit kernel 11.1 us for 128 rows x 32 heads over 512, 13.6 for 256 rows x 28 over
+// 1024 x 4, the token kernel with its merge 11 us for a row of 28 over 32769 x 4 (17.8 MB).
 #include <math.h>
 
 #include "common.h"
@@ -123,7 +129,13 @@ __device__ __forceinline__ int next_visible(const Kv4Params& p, unsigned long lo
 //
 // Eight query tiles (TPW): every wavefront computes and stages an eighth of each
 // tile.  Four: wavefronts 0 .. 3 compute, 4 .. 7 stage.  (Window of 2563 refreshed
-// rows x 32 heads, three rounds of 4: ... us with the computing wavefronts staging.)
+// rows x 32 heads, its store included: 203 us with the computing wavefronts staging,
+// 174 with the idle ones.)
+//
+// What bounds it: matrix (40% of the cycles) and vector work (conversion, exponentials;
+// 24%) of a tile, which partly take turns, and the waits at its barrier; a lane tile
+// does not overlap its two products with the next tile's and takes ~3.4 us, a prefix
+// tile 1.9.
 template <int D, int TPW>
 __global__ __launch_bounds__(K4_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void lane_attn_kv4_kernel(Kv4Params p) {
@@ -529,6 +541,11 @@ void lane_attn_kv4_kernel(Kv4Params p) {
 // takes the 16 bytes of a scale block, converts them and has its operand of four
 // MFMA steps (q's fragments follow the same order of d).  V is converted into an LDS
 // region of the wavefront's own for the transpose reads.
+//
+// What bounds it: latency.  A call with one unit to a wavefront takes 6 us (launch, q,
+// one unit, the combination), every further round of units ~1.2 with an idle chip, 1.7
+// with a workgroup on nearly every compute unit (256 rows x 28 heads over 1024 keys).
+// Codes two or three units ahead do not help.
 template <int D>
 __global__ __launch_bounds__(K4_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void lane_attn_kv4_unit_kernel(Kv4Params p) {
@@ -761,7 +778,8 @@ void lane_attn_kv4_unit_kernel(Kv4Params p) {
 // 1 KB a wavefront; q's fragments follow that order of d.  The scores
 //     S^T = K Q^T: lane (pair, b) has keys 16 t + 4 b + (0..3) of the unit's halves t
 // are the second product's operand as they stand, and V's comes from two transpose
-// reads of those keys' rows.
+// reads of those keys' rows.  (A row of 28 heads over 32769 keys: 8.5 us, 2.1 TB/s, of
+// which ~6 are the chain of one unit; over 131072 keys 18.7 with the merge, 3.8 TB/s.)
 constexpr int K4_TW = 16;   // wavefronts
 template <int D>
 __global__ __launch_bounds__(K4_TW * kWave) void lane_attn_kv4_token_kernel(Kv4Params p) {
