@@ -132,8 +132,8 @@ __device__ __forceinline__ int next_visible(const Kv4Params& p, unsigned long lo
 // rows x 32 heads, its store included: 203 us with the computing wavefronts staging,
 // 174 with the idle ones.)
 //
-// What bounds it: matrix (40% of the cycles) and vector work (conversion, exponentials;
-// 24%) of a tile, which partly take turns, and the waits at its barrier; a lane tile
+// What bounds it: matrix (38% of the cycles) and vector work (conversion, exponentials;
+// 40%) of a tile, which partly take turns, and the waits at its barrier; a lane tile
 // does not overlap its two products with the next tile's and takes ~3.4 us, a prefix
 // tile 1.9.
 template <int D, int TPW>
