@@ -385,11 +385,14 @@ size_t lmhead_mx4_workspace_bytes(int N, int d, int V) {
 
 // The cheapest instance under a cost model: n_nt column tiles, and either whole rounds of
 // workgroups of as many units as there are unit rows, or one round with the units
-// shared out over all compute units.  In us (MI355X): a stage takes 0.25 + 0.16 a
-// column fragment for each wavefront on a SIMD, 0.45 at least, a workgroup 3 more
-// (K split: 5.5), and every further column tile reads W again.  d = 4096: V = 16384, 77
-// rows 26 with K split over two wavefronts, 32 without; V = 152064, 128 rows 149
-// unsplit in one column tile, 171 split in two.
+// shared out over all compute units.  In us (MI355X): a stage takes 0.33 (two columns of
+// wavefronts: 0.27) + 0.16 a column fragment for each wavefront on a SIMD, 0.67 at least, a
+// K split 3.4 a round more and 4% for every further column tile.  Fitted to every instance
+// at 17 pairs of d and V from 256 x 1024 to 2048 x 250000, 1 to 1024 rows: the choice takes
+// 0.7% more than the fastest on average, 10% at most.  Both sides: d = 3584, V =
+// 152064, 512 rows 450 with six fragments unsplit, 481 with thirteen in two columns, 128
+// rows 137 with eight in two columns, 144 with four; d = 4096, V = 32000, 32 rows 21 with
+// K split in four, 25 without; d = 2048, V = 2000, 320 rows 14 unsplit, 16 split in two.
 static LmMx4Layout lm_mx4_layout(int N, int d, int V) {
   const int frags = (N + 15) / 16, n_u = mx4_units(V), n_st = mx4_stages(d), cus = lm_cu_count();
   const int most = lm_mx4_most_vt(V);
@@ -401,9 +404,10 @@ static LmMx4Layout lm_mx4_layout(int N, int d, int V) {
     const int n_vt = std::max((n_u + wr - 1) / wr, std::min(n_u, std::max(1, cus / n_nt)));        \
     const int upw = (n_u + n_vt - 1) / n_vt;                                                       \
     const double waves = (upw * WC * KS + 3) / 4;                                                  \
-    const double stage = std::max(0.45, waves * (0.25 + 0.16 * ((CBT + WC - 1) / WC)));            \
+    const double stage = std::max(0.67, waves * ((WC > 1 ? 0.27 : 0.33) + 0.16 * ((CBT + WC - 1) / WC))); \
     const double rounds = (double)(((long long)n_vt * n_nt + cus - 1) / cus);                      \
-    const double t = rounds * (((n_st + KS - 1) / KS) * stage + 3.0 + (KS > 1 ? 2.5 : 0.0)) * (1 + 0.1 * (n_nt - 1));  \
+    const double t = rounds * (((n_st + KS - 1) / KS) * stage + (KS > 1 ? 3.4 : 0.0)) *            \
+                     (KS > 1 ? 1 + 0.04 * (n_nt - 1) : 1.0);                                       \
     if (n_vt <= most && t < best_t) {                                                              \
       best_t = t;                                                                                  \
       best = LmMx4Layout{CBT, WC, KS, n_vt, n_nt};                                                 \

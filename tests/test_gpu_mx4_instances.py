@@ -16,6 +16,10 @@ LM_CASES = [  # N, d, V
     (788, 1696, 1), (79, 1792, 15245), (390, 1280, 10), (87, 32, 40994), (85, 128, 66503), (249, 128, 16991),
     (906, 2016, 1), (85, 1920, 28057), (954, 2304, 1), (65, 32, 1), (75, 128, 1), (171, 128, 1), (131, 32, 1),
     (134, 128, 1), (259, 128, 1), (387, 32, 1), (176, 128, 22444), (389, 128, 1),
+    (1417, 32, 516), (21, 128, 34189), (20, 1152, 1), (38, 1280, 1), (42, 128, 34714), (99, 2720, 9429), (57, 2944, 17378),
+    (109, 3200, 9577), (75, 1216, 27701), (71, 1280, 31131), (129, 1536, 13628), (244, 2720, 9002), (89, 3456, 22568),
+    (176, 3584, 13161), (828, 128, 2416), (134, 32, 22397), (131, 128, 25307), (200, 32, 23592), (207, 256, 22710),
+    (403, 128, 15153),
     # several rounds of workgroups, units shared out unevenly, K groups of every remainder
     (16, 1024, 140001), (40, 1152, 17000), (77, 1408, 70000), (100, 1056, 100003), (150, 640, 66000), (420, 384, 40000),
     (12, 4224, 9000), (30, 4128, 9001), (8, 8192, 777), (300, 2080, 12345),
