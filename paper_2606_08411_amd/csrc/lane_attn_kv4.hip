@@ -1055,18 +1055,21 @@ struct Kv4Pass {
   size_t ws;
 };
 
+// Tiles of kt keys that n rows make (n up to INT32_MAX: n + kt - 1 would not do).
+static int kv4_tiles(int n, int kt) { return n / kt + (n % kt != 0); }
+
 // R: rows of all lane blocks (0: refreshed rows, which see the prefix alone).
 static Kv4Pass kv4_pass(int n_rows, int R, int P, int Hq, int Hkv, int D) {
   Kv4Pass s{};
   s.n_rows = n_rows;
   s.n_pairs = n_rows * (Hq / Hkv);
   const long long q_tiles = (s.n_pairs + 31) / 32;
-  const int units = (P + K4_UT - 1) / K4_UT + (R + K4_UT - 1) / K4_UT;
+  const int units = kv4_tiles(P, K4_UT) + kv4_tiles(R, K4_UT);
   s.n_split = 1;
   s.token = s.n_pairs <= 16;
   s.units = q_tiles * Hkv <= 256;
   if (s.token) {
-    s.n_pre = (P + K4_UT - 1) / K4_UT;
+    s.n_pre = kv4_tiles(P, K4_UT);
     s.n_tiles = units;
     // One token, 28 heads on 4: 1024 rows 9.7 us unsplit, 11.3 with two splits; 2048 rows 12.7 and
     // 11.4, 3000 rows 15.9 and 11.3 with four (MI355X).  64 splits against 32 (half of the
@@ -1074,12 +1077,12 @@ static Kv4Pass kv4_pass(int n_rows, int R, int P, int Hq, int Hkv, int D) {
     if (units > 3 * K4_TW)
       while (s.n_split < K4_MAX_SPLIT && Hkv * s.n_split * 2 <= 256 && units >= 2 * K4_TW * s.n_split) s.n_split *= 2;
   } else if (s.units) {
-    s.n_pre = (P + K4_UT - 1) / K4_UT;
+    s.n_pre = kv4_tiles(P, K4_UT);
     s.n_tiles = units;
     while (s.n_split < K4_MAX_SPLIT && q_tiles * Hkv * s.n_split * 2 <= 256 && units >= 4 * K4_WAVES * s.n_split) s.n_split *= 2;
   } else {
-    s.n_pre = (P + K4_KT - 1) / K4_KT;
-    s.n_tiles = s.n_pre + (R + K4_KT - 1) / K4_KT;
+    s.n_pre = kv4_tiles(P, K4_KT);
+    s.n_tiles = s.n_pre + kv4_tiles(R, K4_KT);
     // The cheapest of 8 or 4 query tiles a workgroup and 1 to 16 splits, in us
     // (MI355X): a key tile costs 1.9 with 8, 1.1 with 4 (two thirds of it at D = 64), a
     // round of one workgroup per compute unit 5, a split its partials and a merge.

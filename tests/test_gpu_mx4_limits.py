@@ -1,0 +1,54 @@
+"""The 4-bit calls on the GPU at the ends of their ranges."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2606_08411_amd as al
+from gpu_util import dev_bf16
+from mx4_util import EPS32, EPSB, bf16_normal, f64, host_f64
+import synth
+
+pytestmark = pytest.mark.gpu
+
+
+def _room(nbytes):
+    """Skips where the card has not that much memory left."""
+    torch.cuda.empty_cache()
+    free, _ = torch.cuda.mem_get_info()
+    if free < nbytes:
+        pytest.skip(f"needs {nbytes / 1e9:.0f} GB, {free / 1e9:.0f} are free")
+
+
+def test_the_longest_prefix():
+    """One token over INT32_MAX rows: zeros, then a few that take about half of the weight.
+
+    What is off: a score by e (mx4_util.attention_bounds); the sums of the zero keys are whole numbers below
+    2^24 in each wavefront (2^31 keys on 64 splits x 16 wavefronts), so exact, and the joins add at most 16 + 64
+    + 40 roundings; P and the output are rounded to bf16."""
+    P, D, Hq, T = 2 ** 31 - 1, 64, 4, 40
+    _room(2 * P * (D // 2 + D // 32) + (8 << 30))
+    codes = torch.zeros((2, 1, P, D // 2), dtype=torch.uint8, device="cuda")
+    scales = torch.zeros((2, 1, P, D // 32), dtype=torch.uint8, device="cuda")
+    g = np.random.default_rng(2)
+    q = bf16_normal(g, 1, Hq, D)
+    k, v = bf16_normal(g, T, 1, D), bf16_normal(g, T, 1, D)
+    along = f64(q)[0] * (21.5 * D ** 0.5 / (f64(q)[0] ** 2).sum(1, keepdims=True))   # a key along each query, score ~21.5
+    k[-Hq:, 0] = synth.f32_to_bf16_bits(along.astype(np.float32))
+    al.kv4_store(dev_bf16(k), dev_bf16(v), codes, scales, start=P - T)
+    o, lse, _, _ = al.lane_attn_forward_kv4(dev_bf16(q), dev_bf16(k[:1]), dev_bf16(v[:1]), codes, scales, P, [-1], 1)
+    got_o, got_lse = host_f64(o)[0], host_f64(lse)[0]
+    del codes, scales
+    torch.cuda.empty_cache()
+    kk = np.concatenate([oracle.mx4.rounded(f64(k)), f64(k[:1])])[:, 0]
+    vv = np.concatenate([oracle.mx4.rounded(f64(v)), f64(v[:1])])[:, 0]
+    for h in range(Hq):
+        qh = f64(q)[0, h]
+        z = kk @ qh / D ** 0.5
+        total = (P - T) + np.exp(z).sum()
+        e = 2 * D * EPS32 * D ** -0.5 * np.linalg.norm(qh) * np.linalg.norm(kk, axis=1).max()
+        assert 0.05 < np.exp(z).sum() / total < 0.999
+        ref = np.exp(z) @ vv / total
+        mean_abs = np.exp(z) @ np.abs(vv) / total
+        assert (np.abs(got_o[h] - ref) <= 1.01 * (EPSB * np.abs(ref) + (EPSB + 4 * e + 240 * EPS32) * mean_abs)).all()
+        assert abs(got_lse[h] - np.log(total)) <= 2 * e + 120 * EPS32 + 8 * EPS32 * np.log(total)
