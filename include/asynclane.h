@@ -36,6 +36,10 @@
  * - Work is enqueued on `stream` (a hipStream_t; NULL = the null stream) and
  *   the call returns before it completes.  Inputs must stay valid until the
  *   stream reaches that point.
+ * - A call may enqueue several kernels that hand partial results over in its
+ *   workspace.  Calls that share a workspace must follow one another, in their
+ *   enqueueing too: two host threads that call on one stream need a workspace
+ *   each (or a lock around the calls).
  * - Return value: AL_OK (0), or a negative AL_ERR_* status.  Argument errors
  *   are detected before anything is enqueued; AL_ERR_HIP reports a failed
  *   launch (hipGetLastError after the enqueue).  Nothing is printed and no

@@ -242,14 +242,22 @@ def _host_ids(x):
 
 
 # ------------------------------------------------------------ workspaces
-# Default workspaces, one per (kind, device, stream): calls on different
-# streams never share one.  A buffer that has to grow is replaced by one at
-# least twice its size and the old one is kept alive (never returned to the
-# allocator), because a launch still in flight may still write to it.  While
-# a HIP graph is being captured the caller must pass its own workspace, so
+# Default workspaces, one per (thread, kind, device, stream): calls on different
+# streams never share one, nor do calls of two host threads on one stream (a
+# call is several launches: the other thread's may come between its partials
+# and their merge).  A buffer that has to grow is replaced by one at least
+# twice its size and the old one is kept alive while its thread lives.  When a
+# thread ends its buffers go back to torch's allocator, which gives them out
+# again on the same stream only, behind the launches that still use them.
+# While a HIP graph is being captured the caller must pass its own workspace, so
 # no two graphs (or a graph and eager calls) share one by default.
-_ws_cache: dict = {}
-_ws_retired: list = []
+class _ThreadWorkspaces(threading.local):
+    def __init__(self):   # (run in every thread that comes to use it)
+        self.cache: dict = {}
+        self.retired: list = []
+
+
+_ws = _ThreadWorkspaces()
 
 
 def _workspace(kind: str, nbytes: int, device, stream: int):
@@ -259,14 +267,15 @@ def _workspace(kind: str, nbytes: int, device, stream: int):
         raise AsyncLaneError(
             f"{kind}: pass workspace= while a HIP graph is being captured (the call needs "
             f"{nbytes} bytes of workspace)")
+    cache = _ws.cache
     key = (kind, device.index, int(stream))
-    buf = _ws_cache.get(key)
+    buf = cache.get(key)
     if buf is None or buf.numel() < nbytes:
         grow = 0 if buf is None else 2 * buf.numel()
         new = torch.empty(max(nbytes, 256, grow), dtype=torch.uint8, device=device)
         if buf is not None:
-            _ws_retired.append(buf)
-        _ws_cache[key] = buf = new
+            _ws.retired.append(buf)
+        cache[key] = buf = new
     return buf, buf.numel()
 
 
