@@ -39,6 +39,18 @@ _ll = ctypes.c_longlong
 _f = ctypes.c_float
 _sz = ctypes.c_size_t
 
+
+class _Int32:
+    """A 32-bit argument of the library.  (ctypes' own int cuts a number that does
+    not fit down to its low 32 bits: a start of 2^32 rows would be row 0.)"""
+
+    @staticmethod
+    def from_param(v):
+        if not -0x80000000 <= v <= 0x7FFFFFFF:
+            raise OverflowError(f"{v} does not fit a 32-bit integer")
+        return v if type(v) is int else _i.from_param(v)
+
+
 _SIGNATURES = {
     "al_status_string": (ctypes.c_char_p, [_i]),
     "lane_attn_workspace_size": (_sz, [_i] * 7),
@@ -126,7 +138,7 @@ def library() -> ctypes.CDLL:
             for name, (res, args) in _SIGNATURES.items():
                 fn = getattr(lib, name)
                 fn.restype = res
-                fn.argtypes = args
+                fn.argtypes = [_Int32 if a is _i else a for a in args]
             _fast = _load_fast(lib)   # before _lib: callers that see _lib use _fast
             _lib = lib
     return _lib
@@ -178,6 +190,14 @@ def _same_device(*ts):
         raise AsyncLaneError(f"tensors on different devices: {sorted(str(d) for d in devs)}")
 
 
+def _checked(fn, *args):
+    """fn(*args), with the binding's error for an argument that is no 32-bit integer."""
+    try:
+        return fn(*args)
+    except ctypes.ArgumentError as e:
+        raise AsyncLaneError(f"{fn.__name__}: {e}") from None
+
+
 def _call(fn, t, *args):
     """Call library function fn with t's device current: the ABI takes device
     pointers (and the stream) of the current HIP device, and the library's
@@ -186,8 +206,8 @@ def _call(fn, t, *args):
     idx = t.device.index
     if idx is not None and idx != torch.cuda.current_device():
         with torch.cuda.device(idx):
-            return fn(*args)
-    return fn(*args)
+            return _checked(fn, *args)
+    return _checked(fn, *args)
 
 
 # torch's raw-handle accessor costs ~0.1 us against ~3 us for
@@ -289,7 +309,7 @@ def _explicit_workspace(ws, device):
 
 # ------------------------------------------------------------ entry points
 def lane_attn_workspace_size(L, B, P, Hq, Hkv, D, n_refresh=0) -> int:
-    return int(library().lane_attn_workspace_size(L, B, P, Hq, Hkv, D, n_refresh))
+    return int(_checked(library().lane_attn_workspace_size, L, B, P, Hq, Hkv, D, n_refresh))
 
 
 def lane_attn_forward(q, k_lane, v_lane, k_prefix, v_prefix, parent, B, scale=0.0,
@@ -355,7 +375,7 @@ def lane_attn_forward(q, k_lane, v_lane, k_prefix, v_prefix, parent, B, scale=0.
         _tensor(lse_ref, "lse_ref", f32, (n_ref, Hq), optional=True)
     _same_device(q, k_lane, v_lane, k_prefix, v_prefix, o, lse, refresh_idx, q_ref, k_ref,
                  v_ref, o_ref, lse_ref)
-    need = int(lib.lane_attn_workspace_size(L, B, P, Hq, Hkv, D, n_ref))
+    need = int(_checked(lib.lane_attn_workspace_size, L, B, P, Hq, Hkv, D, n_ref))
     if workspace is not None:
         ws, ws_bytes = _explicit_workspace(workspace, dev)
     stream = _stream(k_prefix)
@@ -379,7 +399,7 @@ def al_refresh_window(P, L_gen, lane_start, valid_len, margin) -> int:
     n = len(lane_start)
     s = _host_i32(lane_start, n, "lane_start")
     v = _host_i32(valid_len, n, "valid_len")
-    r = int(library().al_refresh_window(int(P), int(L_gen), _np_ptr(s) if n else None,
+    r = int(_checked(library().al_refresh_window, int(P), int(L_gen), _np_ptr(s) if n else None,
                                         _np_ptr(v) if n else None, n, int(margin)))
     if r < 0:
         _check(r, "al_refresh_window")
@@ -387,7 +407,7 @@ def al_refresh_window(P, L_gen, lane_start, valid_len, margin) -> int:
 
 
 def lmhead_confidence_workspace_size(N, d, V) -> int:
-    return int(library().lmhead_confidence_workspace_size(N, d, V))
+    return int(_checked(library().lmhead_confidence_workspace_size, N, d, V))
 
 
 def _lmhead_args(hidden, W, row_idx, suppress_eos, conf, argmax, lse, want_lse, V=None, mx4=False):
@@ -405,12 +425,12 @@ def _lmhead_args(hidden, W, row_idx, suppress_eos, conf, argmax, lse, want_lse, 
             raise AsyncLaneError(f"W: [V][d={d}] expected, got shape {tuple(W.shape)}")
         V = int(W.shape[0])
     elif mx4:
-        nbytes = int(library().lmhead_packed_weight_mx4_size(int(d), int(V)))
+        nbytes = int(_checked(library().lmhead_packed_weight_mx4_size, int(d), int(V)))
         if nbytes == 0:
             raise AsyncLaneError(f"W_mx4: no packed layout for d={d}, V={V}")
         _tensor(W, "W_mx4", torch.uint8, min_numel=nbytes)
     else:
-        nbytes = int(library().lmhead_packed_weight_size(int(d), int(V)))
+        nbytes = int(_checked(library().lmhead_packed_weight_size, int(d), int(V)))
         if nbytes == 0:
             raise AsyncLaneError(f"W_packed: no packed layout for d={d}, V={V}")
         _tensor(W, "W_packed", bf16, min_numel=nbytes // 2)
@@ -453,7 +473,7 @@ def lmhead_confidence(hidden, W, row_idx=None, suppress_eos=None, eos_id=-1,
     if N == 0:
         return conf, argmax, lse
     dev = hidden.device
-    need = int(lib.lmhead_confidence_workspace_size(N, d, V))
+    need = int(_checked(lib.lmhead_confidence_workspace_size, N, d, V))
     if workspace is not None:
         ws, ws_bytes = _explicit_workspace(workspace, dev)
     stream = _stream(hidden)
@@ -468,7 +488,7 @@ def lmhead_confidence(hidden, W, row_idx=None, suppress_eos=None, eos_id=-1,
 
 
 def lmhead_packed_weight_size(d, V) -> int:
-    return int(library().lmhead_packed_weight_size(int(d), int(V)))
+    return int(_checked(library().lmhead_packed_weight_size, int(d), int(V)))
 
 
 def lmhead_pack_weight(W, out=None):
@@ -480,7 +500,7 @@ def lmhead_pack_weight(W, out=None):
     if W.dim() != 2:
         raise AsyncLaneError(f"W: [V][d] expected, got shape {tuple(W.shape)}")
     V, d = (int(x) for x in W.shape)
-    nbytes = int(lib.lmhead_packed_weight_size(d, V))
+    nbytes = int(_checked(lib.lmhead_packed_weight_size, d, V))
     if nbytes == 0:
         raise AsyncLaneError(f"W: unsupported shape {tuple(W.shape)}")
     if out is None:
@@ -507,7 +527,7 @@ def lmhead_confidence_packed(hidden, W_packed, V, row_idx=None, suppress_eos=Non
     if N == 0:
         return conf, argmax, lse
     dev = hidden.device
-    need = int(lib.lmhead_confidence_workspace_size(N, d, V))
+    need = int(_checked(lib.lmhead_confidence_workspace_size, N, d, V))
     if workspace is not None:
         ws, ws_bytes = _explicit_workspace(workspace, dev)
     stream = _stream(hidden)
@@ -698,7 +718,7 @@ def kv4_store(k, v, kv_codes, kv_scales, row_idx=None, start=0):
 
 
 def lane_attn_kv4_workspace_size(L, B, P, Hq, Hkv, D, n_refresh=0) -> int:
-    return int(library().lane_attn_kv4_workspace_size(L, B, P, Hq, Hkv, D, n_refresh))
+    return int(_checked(library().lane_attn_kv4_workspace_size, L, B, P, Hq, Hkv, D, n_refresh))
 
 
 def lane_attn_forward_kv4(q, k_lane, v_lane, kv_codes, kv_scales, P, parent, B, scale=0.0,
@@ -756,7 +776,7 @@ def lane_attn_forward_kv4(q, k_lane, v_lane, kv_codes, kv_scales, P, parent, B, 
         _tensor(lse_ref, "lse_ref", f32, (n_ref, Hq), optional=True)
     _same_device(q, k_lane, v_lane, kv_codes, kv_scales, o, lse, refresh_idx, q_ref, k_ref, v_ref,
                  o_ref, lse_ref)
-    need = int(lib.lane_attn_kv4_workspace_size(L, B, P, Hq, Hkv, D, n_ref))
+    need = int(_checked(lib.lane_attn_kv4_workspace_size, L, B, P, Hq, Hkv, D, n_ref))
     if workspace is not None:
         ws, ws_bytes = _explicit_workspace(workspace, dev)
     stream = _stream(kv_codes)
@@ -775,7 +795,7 @@ def lane_attn_forward_kv4(q, k_lane, v_lane, kv_codes, kv_scales, P, parent, B, 
 
 
 def lmhead_packed_weight_mx4_size(d, V) -> int:
-    return int(library().lmhead_packed_weight_mx4_size(int(d), int(V)))
+    return int(_checked(library().lmhead_packed_weight_mx4_size, int(d), int(V)))
 
 
 def lmhead_pack_weight_mx4(codes, scales, out=None):
@@ -787,7 +807,7 @@ def lmhead_pack_weight_mx4(codes, scales, out=None):
     if len(lead) != 1:
         raise AsyncLaneError(f"codes: [V][d/2] expected, got shape {tuple(codes.shape)}")
     V = int(lead[0])
-    nbytes = int(lib.lmhead_packed_weight_mx4_size(d, V))
+    nbytes = int(_checked(lib.lmhead_packed_weight_mx4_size, d, V))
     if nbytes == 0:
         raise AsyncLaneError(f"codes: unsupported shape {tuple(codes.shape)}")
     if out is None:
@@ -801,7 +821,7 @@ def lmhead_pack_weight_mx4(codes, scales, out=None):
 
 
 def lmhead_confidence_mx4_workspace_size(N, d, V) -> int:
-    return int(library().lmhead_confidence_mx4_workspace_size(int(N), int(d), int(V)))
+    return int(_checked(library().lmhead_confidence_mx4_workspace_size, int(N), int(d), int(V)))
 
 
 def lmhead_confidence_mx4(hidden, W_mx4, V, row_idx=None, suppress_eos=None, eos_id=-1,
@@ -820,7 +840,7 @@ def lmhead_confidence_mx4(hidden, W_mx4, V, row_idx=None, suppress_eos=None, eos
     if N == 0:
         return conf, argmax, lse
     dev = hidden.device
-    need = int(lib.lmhead_confidence_mx4_workspace_size(N, d, V))
+    need = int(_checked(lib.lmhead_confidence_mx4_workspace_size, N, d, V))
     if workspace is not None:
         ws, ws_bytes = _explicit_workspace(workspace, dev)
     stream = _stream(hidden)
@@ -842,7 +862,7 @@ class AlSched:
     def __init__(self, P, L_gen, B, window=0, max_lanes=64, pad_id=3):
         self._lib = library()
         self.L, self.B, self.W = int(L_gen), int(B), int(B) + int(window)
-        self._h = self._lib.al_sched_create(int(P), int(L_gen), int(B), int(window),
+        self._h = _checked(self._lib.al_sched_create, int(P), int(L_gen), int(B), int(window),
                                             int(max_lanes), int(pad_id))
         if not self._h:
             raise AsyncLaneError("al_sched_create: bad arguments")

@@ -52,3 +52,20 @@ def test_the_longest_prefix():
         mean_abs = np.exp(z) @ np.abs(vv) / total
         assert (np.abs(got_o[h] - ref) <= 1.01 * (EPSB * np.abs(ref) + (EPSB + 4 * e + 240 * EPS32) * mean_abs)).all()
         assert abs(got_lse[h] - np.log(total)) <= 2 * e + 120 * EPS32 + 8 * EPS32 * np.log(total)
+
+
+@pytest.mark.parametrize("n", [2 ** 32, -2 ** 32, 2 ** 31])
+def test_numbers_past_32_bits_are_refused(n):
+    """In the calls themselves; nothing is written."""
+    codes = torch.full((2, 2, 8, 32), 0x5A, dtype=torch.uint8, device="cuda")
+    scales = torch.full((2, 2, 8, 2), 0x5A, dtype=torch.uint8, device="cuda")
+    rows = torch.ones(3, 2, 64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(al.AsyncLaneError, match="kv4_store: .*32-bit"):
+        al.kv4_store(rows, rows, codes, scales, start=n)
+    assert bool((codes == 0x5A).all()) and bool((scales == 0x5A).all())
+    h = torch.ones(3, 64, dtype=torch.bfloat16, device="cuda")
+    W = al.lmhead_pack_weight_mx4(*al.mx4_quantize(torch.ones(100, 64, dtype=torch.bfloat16, device="cuda")))
+    conf = torch.full((3,), 7.0, device="cuda")
+    with pytest.raises(al.AsyncLaneError, match="lmhead_confidence_mx4: .*32-bit"):
+        al.lmhead_confidence_mx4(h, W, 100, eos_id=n, conf=conf)
+    assert bool((conf == 7).all())
