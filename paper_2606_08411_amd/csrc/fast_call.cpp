@@ -12,7 +12,9 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/Context.h>
 #include <ATen/EmptyTensor.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -201,9 +203,13 @@ bool status_ok(int st, const char* what) {
 
 // A new output beside `like`, from the allocator of its storage.  (at::empty finds the
 // same allocator through the dispatcher, 0.3-0.5 us a tensor; a storage without one goes
-// that way.)
+// that way, and so does every output while a dispatch mode watches torch's calls or
+// uninitialised memory is to be filled.)
 at::Tensor fresh(const at::Tensor& like, at::IntArrayRef size, at::ScalarType type) {
-  if (c10::Allocator* const from = like.storage().allocator()) {
+  const at::Context& c = at::globalContext();
+  const bool plain = !c10::impl::dispatch_mode_enabled() &&
+                     !(c.deterministicAlgorithms() && c.deterministicFillUninitializedMemory());
+  if (c10::Allocator* const from = plain ? like.storage().allocator() : nullptr) {
     at::Tensor t(at::detail::empty_generic(size, from, c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt));
     if (t.device() == like.device()) return t;
   }
