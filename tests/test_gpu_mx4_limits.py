@@ -69,3 +69,64 @@ def test_numbers_past_32_bits_are_refused(n):
     with pytest.raises(al.AsyncLaneError, match="lmhead_confidence_mx4: .*32-bit"):
         al.lmhead_confidence_mx4(h, W, 100, eos_id=n, conf=conf)
     assert bool((conf == 7).all())
+
+
+# Sizes past one pass of the kernels' threads (2^20 workgroups of 256 threads; four 8-element segments a thread in the
+# quantiser and its inverse, one in the store): the same rows in calls that take one pass are the reference.
+def _normal_rows(R, n):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(6)
+    x = torch.empty(R, n, dtype=torch.bfloat16, device="cuda")
+    for r in range(0, R, 1 << 17):
+        x[r:r + (1 << 17)].normal_(generator=g)
+    return x
+
+
+def test_quantize_and_read_back_in_two_passes():
+    R, n, step = (1 << 21) + 5, 4096, 1 << 18
+    assert R * n // 8 > (1 << 20) * 256 * 4 >= step * n // 8
+    _room(int(2.2 * R * n * 2.6))
+    x = _normal_rows(R, n)
+    codes, scales = al.mx4_quantize(x)
+    for r in range(0, R, step):
+        c, s = al.mx4_quantize(x[r:r + step])
+        assert torch.equal(codes[r:r + step], c) and torch.equal(scales[r:r + step], s)
+    rc, rs = oracle.mx4.quantize(host_f64(x[-7:]))
+    assert np.array_equal(codes[-7:].cpu().numpy(), rc) and np.array_equal(scales[-7:].cpu().numpy(), rs)
+    del x
+    y = al.mx4_dequantize(codes, scales)
+    for r in range(0, R, step):
+        assert torch.equal(y[r:r + step], al.mx4_dequantize(codes[r:r + step], scales[r:r + step]))
+    assert np.array_equal(host_f64(y[-7:]), oracle.mx4.values(rc, rs))
+
+
+def test_store_in_two_passes():
+    T, Hkv, D = (1 << 21) + 3, 8, 128
+    assert T * Hkv * D // 8 > (1 << 20) * 256
+    _room(16 * T * Hkv * D)
+    k, v = _normal_rows(T * Hkv, D).view(T, Hkv, D), _normal_rows(T * Hkv, D).view(T, Hkv, D).neg()
+    codes = torch.full((2, Hkv, T + 2, D // 2), 0x5A, dtype=torch.uint8, device="cuda")
+    scales = torch.full((2, Hkv, T + 2, D // 32), 0x5A, dtype=torch.uint8, device="cuda")
+    al.kv4_store(k, v, codes, scales, start=1)
+    for plane, x in enumerate((k, v)):
+        c, s = al.mx4_quantize(x)
+        assert torch.equal(codes[plane, :, 1:-1], c.transpose(0, 1))
+        assert torch.equal(scales[plane, :, 1:-1], s.transpose(0, 1))
+    for t in (codes, scales):
+        assert bool((t[:, :, 0] == 0x5A).all()) and bool((t[:, :, -1] == 0x5A).all())
+
+
+@pytest.mark.parametrize("rows", [1 << 15, (1 << 15) + 3])
+def test_read_back_of_large_tensors(rows):
+    """At 2^25 elements and past them, where the values are stored past the caches: every value."""
+    n = 1024
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    codes = torch.randint(0, 256, (rows, n // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.randint(2, 250, (rows, n // 32), generator=g, device="cuda", dtype=torch.uint8)
+    y = al.mx4_dequantize(codes, scales)
+    table = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6, -0., -.5, -1, -1.5, -2, -3, -4, -6], device="cuda")
+    code = torch.stack([codes & 15, codes >> 4], -1).view(rows, n // 32, 32).int()
+    power = (scales.int() << 23).view(torch.float32)   # 2^(s - 127), exactly (torch.ldexp's powf is off by a step for some)
+    want = (table[code] * power[..., None]).view(rows, n)
+    assert torch.equal(y.float(), want)
