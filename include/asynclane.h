@@ -40,6 +40,12 @@
  *   workspace.  Calls that share a workspace must follow one another, in their
  *   enqueueing too: two host threads that call on one stream need a workspace
  *   each (or a lock around the calls).
+ * - A *_workspace_size() is that of its arguments.  The two attention calls split
+ *   the keys less as there is more work, so a smaller call (fewer lanes, a
+ *   shorter prefix) may need more bytes than a larger one, or some where that
+ *   needs none: a workspace that serves several shapes has the largest of
+ *   their sizes, not the size of the largest shape.  (The 4-bit LM head's size
+ *   does not fall as N grows.)
  * - Return value: AL_OK (0), or a negative AL_ERR_* status.  Argument errors
  *   are detected before anything is enqueued; AL_ERR_HIP reports a failed
  *   launch (hipGetLastError after the enqueue).  Nothing is printed and no

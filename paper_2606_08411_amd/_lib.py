@@ -309,6 +309,8 @@ def _explicit_workspace(ws, device):
 
 # ------------------------------------------------------------ entry points
 def lane_attn_workspace_size(L, B, P, Hq, Hkv, D, n_refresh=0) -> int:
+    """Bytes of workspace that a call of these sizes needs.  A smaller call may need
+    more: a workspace for several shapes has the largest of their sizes."""
     return int(_checked(library().lane_attn_workspace_size, L, B, P, Hq, Hkv, D, n_refresh))
 
 
@@ -718,6 +720,8 @@ def kv4_store(k, v, kv_codes, kv_scales, row_idx=None, start=0):
 
 
 def lane_attn_kv4_workspace_size(L, B, P, Hq, Hkv, D, n_refresh=0) -> int:
+    """Bytes of workspace that a call of these sizes needs.  A smaller call may need
+    more: a workspace for several shapes has the largest of their sizes."""
     return int(_checked(library().lane_attn_kv4_workspace_size, L, B, P, Hq, Hkv, D, n_refresh))
 
 
