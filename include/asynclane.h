@@ -51,7 +51,7 @@
  *   launch (hipGetLastError after the enqueue).  Nothing is printed and no
  *   exception crosses the boundary.
  * - Preconditions that are NOT checked: finite inputs; refresh indices unique
- *   and in [0, P); row_idx values in [0, n_rows); row_pos strictly ascending
+ *   and in [0, P) (lane_attn_forward_kv4: unique); row_idx values in [0, n_rows); row_pos strictly ascending
  *   and in [0, L*B); no overlap between output and input buffers unless a
  *   parameter is documented as in/out.
  */

@@ -135,7 +135,9 @@ __device__ __forceinline__ int next_visible(const Kv4Params& p, unsigned long lo
 // What bounds it: matrix (38% of the cycles) and vector work (conversion, exponentials;
 // 40%) of a tile, which partly take turns, and the waits at its barrier; a lane tile
 // does not overlap its two products with the next tile's and takes ~3.4 us, a prefix
-// tile 1.9.
+// tile 1.9.  At D = 128 the first lane tile's rows, loaded before the last prefix tile's
+// softmax, spill registers there (78 with eight query tiles, 46 with four), once a
+// workgroup; neither loop spills.
 template <int D, int TPW>
 __global__ __launch_bounds__(K4_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void lane_attn_kv4_kernel(Kv4Params p) {
@@ -1067,6 +1069,12 @@ static Kv4Pass kv4_pass(int n_rows, int R, int P, int Hq, int Hkv, int D) {
   const int units = kv4_tiles(P, K4_UT) + kv4_tiles(R, K4_UT);
   s.n_split = 1;
   s.token = s.n_pairs <= 16;
+  // Up to a workgroup of the unit kernel per compute unit.  It converts the keys for every query
+  // tile, the tile kernel once for 8 or 4 of them, so the limit also depends a little on the
+  // length.  Unit and tile kernel (MI355X, us, D = 128; at D = 64 the ratios are the same) over
+  // 512, 4096, 16384 and 32768 keys: 128 rows x 32 heads (128 query tiles) 10.7 17.7, 20.8 28.2, 48.6
+  // 51.4, 86.9 86.9; 256 rows x 28 heads on 4 (224) 11.2 19.7, 26.3 33.1, 78.9 79.9, 149 133; 384 rows
+  // (336, past the limit) 19.4 21.1, 49.8 50.4, 154 126, 295 223; at 1024 keys 23.6 28.0.
   s.units = q_tiles * Hkv <= 256;
   if (s.token) {
     s.n_pre = kv4_tiles(P, K4_UT);

@@ -314,6 +314,8 @@ __global__ __launch_bounds__(512) void lmhead_mx4_kernel(LmMx4Params p) {
 // ------------------------------------------------------------------ pack
 // One 16-byte segment of codes per thread (lane 16 b + r of unit-quarter uq, stage
 // c: row 16 uq + r, bytes 64 c + 16 b), then one dword of scales (the four quarters).
+// A wavefront reads 64 bytes of each of 16 rows and writes 1 KB.  Once at load time, bound by those
+// short reads: 126464 x 4096 in 166 us, 3.3 TB/s read and written (a copy 5.1), 152064 x 3584 in 188.
 __global__ __launch_bounds__(256) void lmhead_pack_mx4_kernel(const uint8_t* codes, const uint8_t* scales, int d, int V,
                                                               int n_u, int n_st, uint8_t* out) {
   const long long n_seg = (long long)n_st * n_u * 256, n_sc = (long long)n_st * n_u * 64;
